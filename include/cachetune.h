@@ -392,6 +392,84 @@ ct_status ct_select_frequency(const void* k, const void* v, int32_t n_batch, int
                               int32_t row_elems, double alpha, double ratio, int32_t* idx_out, float* scores,
                               void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Packed K/V caches: pools and running requests that are held in 4 or 8 bits. ----
+ *
+ * A packed cache is one device allocation of ct_packed_kv_bytes(cfg, n_rows, bits) bytes, 16-byte aligned, that holds
+ * K and V of n_rows token rows (a multiple of 32).  Every 32 consecutive elements of a head row share a scale 2^e,
+ * e the smallest integer >= -117 with max |x| <= 1.75 * 2^emax * 2^e; an element is stored as x / 2^e rounded to nearest
+ * (ties to the even code):
+ *   bits 4   to one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign (e2m1; emax 2)
+ *   bits 8   to three mantissa bits, at most 448, steps of 2^-9 at least, and a sign (e4m3; emax 8)
+ * (magnitudes above 1.75 * 2^127 count as that, so that finite elements come back finite).  4.25 and 8.25 bits per
+ * element with the scales.  32 elements that hold an infinity or a NaN read back as NaN, all
+ * of them.  The bytes of 32 consecutive rows from a multiple of 32 on are contiguous, so such runs may be moved by plain
+ * copies of n / n_rows of the cache's bytes, between devices and host pools too; the layout inside is the
+ * library's own.  A cache's bytes are undefined until rows are written; only rows that were written may be read. */
+
+/* Bytes of a packed cache; 0 for invalid arguments.  Host function. */
+size_t ct_packed_kv_bytes(const ct_layer_cfg* cfg, int32_t n_rows, int32_t bits);
+
+/* Rows t in [0, n_tokens) of k and v are written to cache row rows[t], or first_row + t where rows is NULL.
+ *   k, v     device bf16; row t at element offset t * k_stride (v_stride), [n_kv_heads, head_dim] dense within a row;
+ *            strides of at least a row and multiples of 8: the rows may be part of projected [q|k|v] rows
+ *   rows     device int32 [n_tokens] or NULL; entries outside [0, n_rows) leave their token out (padding); entries
+ *            must differ from one another otherwise (of two equal ones, bytes of both would stay)
+ *   cache    device, 16-byte aligned; rows that are not written keep their bytes
+ * k, v and cache 16-byte aligned (CT_ERR_UNSUPPORTED).  first_row + n_tokens must not pass n_rows (CT_ERR_INDEX).
+ * n_tokens = 0 is legal and does nothing. */
+ct_status ct_pack_kv(const ct_layer_cfg* cfg, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                     int32_t n_tokens, const int32_t* rows, int32_t first_row, void* cache, int32_t n_rows, int32_t bits,
+                     void* stream);
+
+/* The way back: cache row rows[t] (first_row + t where rows is NULL) becomes row t of k_dst and v_dst, its keys rotated
+ * by (new_pos[t] - old_pos[t]) * omega_j as in ct_rerope_keys (Eq. 8) before the one rounding to bf16.  One call puts a
+ * context together from chunks that lie anywhere in the cache.
+ *   rows     device int32 [n_tokens] or NULL; entries outside [0, n_rows) leave row t of k_dst and v_dst as it is
+ *            (rows of the recompute set, which the scatter writes); the same row may be read more than once
+ *   old_pos  device int32 [n_tokens] or NULL (= all zero: a raw pre-RoPE cache)
+ *   new_pos  device int32 [n_tokens] or NULL (no rotation; old_pos must be NULL then)
+ *   k_dst, v_dst  device bf16 [n_tokens, n_kv_heads, head_dim], 16-byte aligned, not overlapping the cache */
+ct_status ct_unpack_kv(const ct_layer_cfg* cfg, const void* cache, int32_t n_rows, int32_t bits, const int32_t* rows,
+                       int32_t first_row, const int32_t* old_pos, const int32_t* new_pos, int32_t n_tokens, void* k_dst,
+                       void* v_dst, void* stream);
+
+/* Attention of the n_new newest tokens of each of n_seq sequences over their packed caches: decoding (n_new = 1) and
+ * the check of drafted tokens.  Sequence b is the cache rows [seq_start[b], seq_start[b] + seq_len[b]), its newest
+ * tokens among them (written before by ct_pack_kv); token t of them sees the first seq_len[b] - n_new + t + 1 rows:
+ *   out[b,t,h,:] = sum_j softmax_j(q[b,t,h,:] . k_j,g * scale) v_j,g,  g = h / (n_q_heads / n_kv_heads).
+ * bf16 operands (the cache's values are exact in bf16), fp32 scores / softmax / accumulation.  A token that sees no
+ * row (an empty sequence, or n_new above its length) gets zeros and lse = -inf.  Rows outside a sequence do not
+ * reach its results, whatever they hold, and neither do rows that a token does not see.
+ *   q, out     device bf16 [n_seq, n_new, n_q_heads, head_dim], 16-byte aligned; n_new in [1, 64]
+ *   seq_start  device int32 [n_seq], any row of the cache
+ *   seq_len    device int32 [n_seq], in [0, max_len]; larger ones are cut to max_len and to the end of the cache
+ *   max_len    host bound of the lengths, at most n_rows; the key range is divided over workgroups for this length
+ *   lse        device fp32 [n_seq, n_new, n_q_heads] natural-log sum-exp of the scaled scores, or NULL
+ *   workspace  device scratch of at least ct_packed_attention_workspace_bytes() bytes, 256-byte aligned (none where
+ *              that is 0); calls that overlap in time need one each
+ * The result of a call does not depend on what else runs; it depends on max_len, n_seq and n_new in the order of its
+ * fp32 sums.  n_seq = 0 is legal and does nothing. */
+ct_status ct_packed_attention(const ct_layer_cfg* cfg, const void* q, int32_t n_seq, int32_t n_new, const void* cache,
+                              int32_t n_rows, int32_t bits, const int32_t* seq_start, const int32_t* seq_len, int32_t max_len,
+                              void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+/* Scratch bytes of that call; 0 where it needs none and for invalid arguments.  Host function. */
+size_t ct_packed_attention_workspace_bytes(const ct_layer_cfg* cfg, int32_t n_seq, int32_t n_new, int32_t max_len);
+
+/* Queries and keys normed head by head, then rotated, for models that norm them before RoPE (ct_qkv_selected rotates
+ * in its epilogue and cannot): the projection is a ct_linear with wqkv, this call takes its rows apart.
+ * For every q and k head x of a row: y = x / sqrt(mean(x^2) + eps) * weight, then RoPE at pos[t]; fp32 arithmetic (angle
+ * reduced in fp64), one rounding to bf16.  v heads are copied.
+ *   qkv       device bf16 [n_tokens, (n_q_heads + 2 n_kv_heads) * head_dim]: q heads, k heads, v heads
+ *   pos       device int32 [n_tokens]
+ *   q_weight, k_weight  device bf16 [head_dim]
+ *   q_out     device bf16 [n_tokens, n_q_heads, head_dim]
+ *   k_out     device bf16 [n_tokens, n_kv_heads, head_dim]
+ *   v_out     the same, or NULL: the values are not copied (ct_pack_kv takes them out of qkv itself)
+ * All 16-byte aligned; outputs may not overlap qkv.  eps >= 0.  n_tokens = 0 is legal and does nothing. */
+ct_status ct_qk_norm_rope(const ct_layer_cfg* cfg, const void* qkv, const int32_t* pos, int32_t n_tokens,
+                          const void* q_weight, const void* k_weight, float eps, void* q_out, void* k_out, void* v_out,
+                          void* stream);
+
 /* Host-side check of an index set: strictly ascending and inside [0, n_ctx). */
 ct_status ct_validate_indices(const int32_t* host_idx, int32_t n_sel, int32_t n_ctx);
 
@@ -402,7 +480,8 @@ ct_status ct_validate_indices(const int32_t* host_idx, int32_t n_sel, int32_t n_
  * times and returns the number of launches and the summed milliseconds; ct_profile_reset
  * forgets what was recorded.  Classes: 0 qkv projection, 1 re-RoPE, 2 scatter,
  * 3 selected attention (main kernel), 4 attention split merge, 5 linear / SwiGLU GEMMs,
- * 6 RMSNorm, 7 frequency scores, 8 TopK.  Profiling is process wide,
+ * 6 RMSNorm and query/key norms, 7 frequency scores, 8 TopK, 9 packing and
+ * unpacking of caches, 10 attention over packed caches (the merge of its parts: 4).  Profiling is process wide,
  * off by default, creates events on first use and is not meant for concurrent callers. */
 void ct_set_profiling(int32_t on);
 void ct_profile_reset(void);

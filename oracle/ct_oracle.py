@@ -40,6 +40,10 @@ intermediate rounding:
                       per-token norms (Eq. 5), joint score (Eq. 6), TopK (Eq. 7).  NumPy's FFT
                       is the library step; everything else is the equations as written.
 
+  packed_values, packed_attention, qk_norm_rope
+                      what goes beyond the paper's layer: the values that a cache held in 4 or 8 bits stands
+                      for, attention of a sequence's newest tokens, per-head norms of q and k before RoPE.
+
 Readings where the paper is silent (RoPE pair convention and frequencies, softmax scale,
 GQA head mapping, floor for r*N, V being position independent) are stated at the function
 that uses them.  All pins live in tests/test_oracle_pins.py.
@@ -360,3 +364,76 @@ def select_frequency(k, v, alpha: float, ratio: float):
     if ratio > 0.0 and n_sel < 1:
         n_sel = 1
     return topk_indices(s, n_sel), s
+
+
+# ----------------------------------------------------------------------------- packed caches, per-head norms
+PACK_GROUP = 32
+
+
+def packed_code_values(bits: int) -> np.ndarray:
+    """The magnitudes that a code stands for, in units of the group's scale, ascending (place = code)."""
+    if bits == 4:
+        return np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+    return np.array([m / 512 for m in range(8)] + [(1 + m / 8) * 2.0 ** e for e in range(-6, 9) for m in range(8)][:-1])
+
+
+def packed_scale_exponent(top, bits: int):
+    """e of the scale 2^e of groups whose largest magnitudes are `top`: the smallest integer >= -117 with
+    top <= 1.75 * 2^emax * 2^e."""
+    top = np.asarray(top, dtype=np.float64)
+    limit = 7.0 if bits == 4 else 448.0
+    e = np.full(top.shape, -117, dtype=np.int64)
+    for k in range(-117, 128):
+        e = np.where(top > limit * 2.0 ** k, k + 1, e)
+    return e
+
+
+def packed_values(x, bits: int):
+    """What rows x [..., D] come back as from a packed cache: per 32 consecutive elements x / 2^e rounded to the nearest
+    code value, ties to the even code; magnitudes above 1.75 * 2^127 count as that.  Groups that hold an infinity or a NaN
+    are NaN."""
+    x = np.asarray(x, dtype=np.float64)
+    values = packed_code_values(bits)
+    g = x.reshape(*x.shape[:-1], x.shape[-1] // PACK_GROUP, PACK_GROUP)
+    bad = ~np.isfinite(g).all(-1, keepdims=True)
+    a = np.where(bad, 0.0, np.minimum(np.abs(np.where(np.isfinite(g), g, 0.0)), 1.75 * 2.0 ** 127))
+    scale = 2.0 ** packed_scale_exponent(a.max(-1, keepdims=True), bits)
+    a = a / scale
+    hi = np.minimum(np.searchsorted(values, a), values.size - 1)
+    lo = np.maximum(hi - 1, 0)
+    up, down = np.abs(values[hi] - a), np.abs(a - values[lo])
+    pick = np.where(up < down, hi, np.where(down < up, lo, np.where(hi % 2 == 0, hi, lo)))
+    out = np.where(np.signbit(g), -1.0, 1.0) * values[pick] * scale
+    return np.where(bad, np.nan, out).reshape(x.shape)
+
+
+def packed_attention(q, k, v, scale=None):
+    """Attention of the newest tokens of ONE sequence: q [n_new, Hq, D], k and v [len, Hkv, D] (the values that the
+    cache stands for).  Token t sees the first len - n_new + t + 1 keys; a token that sees none gets zeros and -inf.
+    Returns (out, lse, weight): weight = sum_j p_j |v_j|, what errors of single probabilities scale with."""
+    q, k, v = (np.asarray(a, dtype=np.float64) for a in (q, k, v))
+    n_new, hq, d = q.shape
+    n, hkv, _ = k.shape
+    scale = 1.0 / np.sqrt(d) if scale is None else scale
+    out, weight = np.zeros((n_new, hq, d)), np.zeros((n_new, hq, d))
+    lse = np.full((n_new, hq), -np.inf)
+    for t in range(n_new):
+        seen = n - n_new + t + 1
+        if seen <= 0:
+            continue
+        for h in range(hq):
+            kg, vg = k[:seen, h // (hq // hkv)], v[:seen, h // (hq // hkv)]
+            s = kg @ q[t, h] * scale
+            p = np.exp(s - s.max())
+            out[t, h] = p @ vg / p.sum()
+            weight[t, h] = p @ np.abs(vg) / p.sum()
+            lse[t, h] = s.max() + np.log(p.sum())
+    return out, lse, weight
+
+
+def qk_norm_rope(qkv, pos, q_weight, k_weight, eps, n_q_heads, n_kv_heads, head_dim, theta, style: int = HALF_SPLIT):
+    """Rows [q heads | k heads | v heads]: q and k heads x / sqrt(mean(x^2) + eps) * weight, then RoPE at pos[t].
+    Returns (q, k, v)."""
+    x = np.asarray(qkv, dtype=np.float64).reshape(len(pos), n_q_heads + 2 * n_kv_heads, head_dim)
+    q, k, v = x[:, :n_q_heads], x[:, n_q_heads:n_q_heads + n_kv_heads], x[:, n_q_heads + n_kv_heads:]
+    return (rotate(rmsnorm(q, q_weight, eps), pos, theta, style), rotate(rmsnorm(k, k_weight, eps), pos, theta, style), v)

@@ -18,7 +18,8 @@ CT_OK = 0
 CT_ERR_NULL, CT_ERR_SHAPE, CT_ERR_INDEX, CT_ERR_RATIO = -1, -2, -3, -4
 CT_ERR_WORKSPACE, CT_ERR_HIP, CT_ERR_UNSUPPORTED = -5, -6, -7
 
-KERNEL_CLASSES = {"qkv": 0, "rerope": 1, "scatter": 2, "attention": 3, "merge": 4, "linear": 5, "norm": 6, "frequency": 7, "topk": 8}
+KERNEL_CLASSES = {"qkv": 0, "rerope": 1, "scatter": 2, "attention": 3, "merge": 4, "linear": 5, "norm": 6, "frequency": 7, "topk": 8,
+                  "pack": 9, "packed_attention": 10}
 
 EXPORTS = [
     "ct_qkv_selected", "ct_rerope_keys", "ct_rerope_keys_skip", "ct_rerope_chunk", "ct_scatter_kv", "ct_selected_attention",
@@ -29,6 +30,8 @@ EXPORTS = [
     "ct_measure_mfma_rate", "ct_layer_latency_model", "ct_ratio_prior", "ct_ratio_search",
     "ct_frequency_scores", "ct_frequency_workspace_bytes", "ct_topk_indices", "ct_frequency_n_selected",
     "ct_select_frequency",
+    "ct_packed_kv_bytes", "ct_pack_kv", "ct_unpack_kv", "ct_packed_attention", "ct_packed_attention_workspace_bytes",
+    "ct_qk_norm_rope",
 ]
 
 
@@ -128,11 +131,20 @@ def load() -> ctypes.CDLL:
     lib.ct_ratio_search.restype = c_int32
     lib.ct_measure_mfma_rate.argtypes = [c_void_p, c_int32, c_void_p, POINTER(c_double)]
     lib.ct_measure_mfma_rate.restype = c_int32
+    lib.ct_packed_kv_bytes.argtypes = [cfgp, c_int32, c_int32]
+    lib.ct_packed_kv_bytes.restype = c_size_t
+    lib.ct_pack_kv.argtypes = [cfgp, P, c_int64, P, c_int64, c_int32, P, c_int32, P, c_int32, c_int32, P]
+    lib.ct_unpack_kv.argtypes = [cfgp, P, c_int32, c_int32, P, c_int32, P, P, c_int32, P, P, P]
+    lib.ct_packed_attention.argtypes = [cfgp, P, c_int32, c_int32, P, c_int32, c_int32, P, P, c_int32, P, P, P, c_size_t, P]
+    lib.ct_packed_attention_workspace_bytes.argtypes = [cfgp, c_int32, c_int32, c_int32]
+    lib.ct_packed_attention_workspace_bytes.restype = c_size_t
+    lib.ct_qk_norm_rope.argtypes = [cfgp, P, P, c_int32, P, P, c_float, P, P, P, P]
     lib.ct_last_error.restype = c_char_p
     lib.ct_version.restype = c_char_p
     for name in ("ct_qkv_selected", "ct_rerope_keys", "ct_rerope_keys_skip", "ct_linear_ws_cus", "ct_rerope_chunk", "ct_scatter_kv", "ct_selected_attention",
                  "ct_partial_prefill_layer", "ct_validate_indices", "ct_profile_read", "ct_rmsnorm", "ct_linear",
-                 "ct_linear_ws", "ct_swiglu", "ct_partial_prefill_stack"):
+                 "ct_linear_ws", "ct_swiglu", "ct_partial_prefill_stack", "ct_pack_kv", "ct_unpack_kv", "ct_packed_attention",
+                 "ct_qk_norm_rope"):
         getattr(lib, name).restype = c_int32
     _lib = lib
     return lib
@@ -356,6 +368,36 @@ def ct_select_frequency(k, v, n_batch, batch_stride, n_tokens, row_elems, alpha,
                         workspace_bytes, stream=None):
     _check(load().ct_select_frequency(_ptr(k), _ptr(v), n_batch, batch_stride, n_tokens, row_elems, alpha, ratio,
                                       _ptr(idx_out), _ptr(scores), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ct_packed_kv_bytes(cfg: LayerCfg, n_rows: int, bits: int) -> int:
+    return int(load().ct_packed_kv_bytes(byref(cfg), n_rows, bits))
+
+
+def ct_pack_kv(cfg, k, k_stride, v, v_stride, n_tokens, rows, first_row, cache, n_rows, bits, stream=None) -> None:
+    _check(load().ct_pack_kv(byref(cfg), _ptr(k), k_stride, _ptr(v), v_stride, n_tokens, _ptr(rows), first_row, _ptr(cache),
+                             n_rows, bits, _stream(stream)))
+
+
+def ct_unpack_kv(cfg, cache, n_rows, bits, rows, first_row, old_pos, new_pos, n_tokens, k_dst, v_dst, stream=None) -> None:
+    _check(load().ct_unpack_kv(byref(cfg), _ptr(cache), n_rows, bits, _ptr(rows), first_row, _ptr(old_pos), _ptr(new_pos),
+                               n_tokens, _ptr(k_dst), _ptr(v_dst), _stream(stream)))
+
+
+def ct_packed_attention_workspace_bytes(cfg: LayerCfg, n_seq: int, n_new: int, max_len: int) -> int:
+    return int(load().ct_packed_attention_workspace_bytes(byref(cfg), n_seq, n_new, max_len))
+
+
+def ct_packed_attention(cfg, q, n_seq, n_new, cache, n_rows, bits, seq_start, seq_len, max_len, out, lse, workspace,
+                        workspace_bytes, stream=None) -> None:
+    _check(load().ct_packed_attention(byref(cfg), _ptr(q), n_seq, n_new, _ptr(cache), n_rows, bits, _ptr(seq_start),
+                                      _ptr(seq_len), max_len, _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes,
+                                      _stream(stream)))
+
+
+def ct_qk_norm_rope(cfg, qkv, pos, n_tokens, q_weight, k_weight, eps, q_out, k_out, v_out, stream=None) -> None:
+    _check(load().ct_qk_norm_rope(byref(cfg), _ptr(qkv), _ptr(pos), n_tokens, _ptr(q_weight), _ptr(k_weight), float(eps),
+                                  _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(stream)))
 
 
 def ct_layer_latency_model(r, n_tokens, t_c, t_i, t_o) -> float:

@@ -19,7 +19,7 @@ constexpr int kNumXCDs = 8;     // accelerator dies; consecutive workgroup ids o
 constexpr int kCUsHeldPerStreamInBlock = 4;
 
 // ---- kernel classes for the opt-in event profiling ------------------------------------
-enum KernelClass { KC_QKV = 0, KC_REROPE = 1, KC_SCATTER = 2, KC_ATTN = 3, KC_MERGE = 4, KC_LINEAR = 5, KC_NORM = 6, KC_FREQ = 7, KC_TOPK = 8, KC_COUNT = 9 };
+enum KernelClass { KC_QKV = 0, KC_REROPE = 1, KC_SCATTER = 2, KC_ATTN = 3, KC_MERGE = 4, KC_LINEAR = 5, KC_NORM = 6, KC_FREQ = 7, KC_TOPK = 8, KC_PACK = 9, KC_PACKED_ATTN = 10, KC_COUNT = 11 };
 
 ct_status fail(ct_status code, const char* fmt, ...);
 ct_status hip_fail(hipError_t e, const char* what);
@@ -171,6 +171,8 @@ ct_status launch_attention(const ct_layer_cfg* cfg, const AttnPlan& plan, const 
                            void* workspace, hipStream_t s, int32_t key_after = 0, int32_t key_upto = 0x7fffffff,
                            float* state = nullptr);
 size_t attention_state_bytes(const ct_layer_cfg* cfg, int n_ctx, int n_sel);
+// What every entry point over a packed cache checks first: the configuration, bits and the number of rows.
+ct_status check_packed(const ct_layer_cfg* cfg, int32_t n_rows, int32_t bits);
 
 }  // namespace ct
 

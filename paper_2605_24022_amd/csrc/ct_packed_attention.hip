@@ -1,0 +1,553 @@
+// Attention of the newest tokens of each sequence over a packed K/V cache (ct_packed_attention): the steps that follow
+// a partial prefill, one token (or a few drafted ones) per sequence at a time.
+//
+// Bound: the cache is read once and used for few queries, so memory decides as long as the conversion of the codes
+// keeps up: an element costs one conversion instruction per two, and V one v_perm per two besides.
+//
+// Formulation, as in the selected-row attention: S^T = K Q^T and O^T += V^T P^T on 16 x 16 x 32 matrix instructions,
+// the columns being the G query heads of a KV head times the new tokens.  The cache's layout hands a lane its
+// operands directly (ct_packed.h): nothing of K, V or P goes through LDS, and the waves of a workgroup walk
+// alternate blocks of 32 keys without waiting for one another; they are joined once, at the end.  Key order within a
+// block: lane row h takes keys 8h .. 8h + 7, in S^T as the rows 4h .. 4h + 3 of two 16-key tiles, which makes the
+// scores of a lane the B operand of the PV step.
+#include <type_traits>
+#include <utility>
+
+#include "ct_packed.h"
+
+namespace ct {
+
+namespace {
+
+constexpr int kWaves = 4;
+
+struct PackedAttnArgs {
+  const uint16_t* q;              // [n_seq, n_new, Hq, D]
+  const unsigned char* cache;
+  const int32_t* seq_start;
+  const int32_t* seq_len;
+  uint16_t* out;
+  float* lse;
+  float* partial;                 // per (sequence, KV head, part): O [C][D], then m [C], l [C]
+  int32_t n_seq, n_new, n_rows, max_len;
+  int32_t Hq, Hkv, group_shift;   // query heads per KV head: 1 << group_shift
+  int32_t n_parts, part_blocks;   // parts of the key range, and blocks of 32 rows in each
+  int32_t col_blocks;
+  float scale_log2;               // softmax scale * log2(e)
+};
+
+// The rows of sequence b in the cache, and the parts its blocks are divided into.  Lengths and starts that do not
+// fit the cache are cut to it.
+struct Sequence {
+  int64_t first, end;   // rows [first, end)
+  int32_t b0, b1;       // blocks [b0, b1)
+  int32_t n_parts;
+};
+__device__ __forceinline__ Sequence sequence_of(const PackedAttnArgs& a, int b) {
+  Sequence s;
+  const int64_t start = a.seq_start[b], len = min(a.seq_len[b], a.max_len);
+  s.first = start;
+  s.end = min(start + len, (int64_t)a.n_rows);
+  if (start < 0 || s.end <= start) s.first = s.end = 0;
+  s.b0 = (int32_t)(s.first / kPackRows);
+  s.b1 = (int32_t)((s.end + kPackRows - 1) / kPackRows);
+  s.n_parts = (s.b1 - s.b0 + a.part_blocks - 1) / a.part_blocks;
+  return s;
+}
+
+template <int N, typename F, int... I>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for_impl<N>(f, std::make_integer_sequence<int, N>{});
+}
+
+// Over the four 16-lane rows of a wave.
+template <typename Op>
+__device__ __forceinline__ float reduce_rows_one(float x, Op op) {
+  uint32_t u = __float_as_uint(x);
+  auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  u = __float_as_uint(op(__uint_as_float(r[0]), __uint_as_float(r[1])));
+  r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// What a lane holds of one block of 32 rows.
+template <int D, int BITS>
+struct Raw {
+  static constexpr int KW = D / 4 * BITS / 32;    // words of one K row
+  static constexpr int VW = D / 16 * BITS / 4;    // words of 8 keys x D / 16 dimensions of V
+  uint32_t k[2][KW];
+  uint32_t v[VW];
+  uint32_t ks;      // two scale bytes
+  uint32_t vs[2];   // eight
+};
+
+template <int W>
+__device__ __forceinline__ void load_words(uint32_t (&dst)[W], const unsigned char* p) {
+  if constexpr (W % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(p + 4 * i);
+      dst[i] = x[0]; dst[i + 1] = x[1]; dst[i + 2] = x[2]; dst[i + 3] = x[3];
+    }
+  } else {
+    static_assert(W == 2, "words per lane");
+    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+    dst[0] = x[0]; dst[1] = x[1];
+  }
+}
+
+// Pair e2 (dimensions 2 e2, 2 e2 + 1 of the lane's) of key s.
+template <int D, int BITS, int S, int E2>
+__device__ __forceinline__ uint32_t v_pair(const uint32_t* v, float scale) {
+  constexpr int byte = (S * (D / 16) + 2 * E2) * BITS / 8;
+  return unpack_pair<BITS, BITS == 4 ? byte % 4 : byte % 4 / 2>(v[byte / 4], scale);
+}
+
+template <int D, int BITS, int NT>
+__global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(PackedAttnArgs a) {
+  using L = PackLayout<D, BITS>;
+  using R = Raw<D, BITS>;
+  constexpr int KS = D / 32;
+  constexpr int MT = L::kLaneDims;      // O^T tiles: row j of tile m is dimension j * MT + m
+  const int lane = threadIdx.x & 63, l16 = lane & 15, h = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  const int g = blockIdx.x % a.Hkv;
+  int rest = blockIdx.x / a.Hkv;
+  const int cb = rest % a.col_blocks;
+  rest /= a.col_blocks;
+  const int part = rest % a.n_parts;
+  const int b = rest / a.n_parts;
+  const Sequence seq = sequence_of(a, b);
+  if (part >= max(seq.n_parts, 1)) return;            // (an empty sequence still gets its zeros, from part 0)
+  const int blk0 = seq.b0 + part * a.part_blocks, blk1 = min(blk0 + a.part_blocks, seq.b1);
+
+  // ---- this lane's columns: column c is head c mod G of new token c / G --------------------------------
+  const int G = 1 << a.group_shift;
+  const int n_cols = a.n_new << a.group_shift;
+  const int col0 = cb * 16 * NT;
+  bf16x8 qf[NT][KS];
+  int64_t last[NT];                                   // the last row that the column sees
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int c = min(col0 + 16 * n + l16, n_cols - 1);
+    const int t = c >> a.group_shift;
+    last[n] = seq.end - a.n_new + t;
+    const uint16_t* qp = a.q + (((int64_t)b * a.n_new + t) * a.Hq + g * G + (c & (G - 1))) * D + h * (D / 4);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[n][ks] = *reinterpret_cast<const bf16x8*>(qp + 8 * ks);
+  }
+  const int64_t first_last = seq.end - a.n_new + (col0 >> a.group_shift);   // the lowest of `last`
+
+  // ---- where a lane finds its share of a block -------------------------------------------------------
+  const int k_row = 8 * (l16 >> 2) + (l16 & 3);       // row of 16-key tile 0; tile 1: 4 rows further on
+  const int k_off = k_row * L::kRowBytes + h * (L::kRowBytes / 4);
+  const int out_group = h * (D / 4) / kPackGroup;     // scale group of the K dimensions, and of the output dimensions
+  const int ks_off = L::kKScales + out_group * kPackRows + 2 * l16;
+  const int v_off = L::kVCodes + (h * 16 + l16) * 8 * L::kLaneBytes;
+  const int vs_off = L::kVScales + l16 * MT / kPackGroup * kPackRows + 8 * h;
+  auto block_ptr = [&](int blk) __attribute__((always_inline)) {
+    return a.cache + ((int64_t)blk * a.Hkv + g) * L::kBytes;
+  };
+  auto load = [&](R& r, int blk) __attribute__((always_inline)) {
+    const unsigned char* p = block_ptr(blk);
+    load_words(r.k[0], p + k_off);
+    load_words(r.k[1], p + k_off + 4 * L::kRowBytes);
+    r.ks = *reinterpret_cast<const uint16_t*>(p + ks_off);
+    load_words(r.v, p + v_off);
+    load_words(r.vs, p + vs_off);
+  };
+
+  // ---- state -----------------------------------------------------------------------------------------
+  f32x4 o[MT][NT];
+  float m_run[NT], m_limit[NT], l_run[NT];
+  const float limit_step = 8.0f / a.scale_log2;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    m_run[n] = m_limit[n] = -INFINITY;
+    l_run[n] = 0.f;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) o[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  auto compute = [&](R& r, int blk) __attribute__((always_inline)) {
+    // scores
+    f32x4 s[2][NT];
+    const float k_scale[2] = {__uint_as_float((r.ks << 23) & 0x7f800000u), __uint_as_float((r.ks << 15) & 0x7f800000u)};
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x4 kw = unpack8<BITS>(&r.k[u][ks * BITS / 4], k_scale[u]);
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, kw);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+          s[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][ks], ks == 0 ? zero : s[u][n], 0, 0, 0);
+        }
+      }
+    // Blocks that reach over an end of the sequence, or past the earliest of the new tokens: rows outside the
+    // sequence may hold anything, rows that only some columns see may hold NaN.
+    const int64_t row0 = (int64_t)blk * kPackRows;
+    if (row0 < seq.first || row0 + kPackRows - 1 > first_last) {
+      const int lo = (int)max(seq.first - row0 - 8 * h, (int64_t)0);         // keys [lo, hi) of the lane's eight are rows
+      const int hi = (int)min(seq.end - row0 - 8 * h, (int64_t)8);           // of the sequence
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int rel = (int)min(last[n] - row0 - 8 * h, (int64_t)8);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            s[u][n][i] = 4 * u + i < lo || 4 * u + i > rel ? -INFINITY : s[u][n][i];
+      }
+      // A probability of zero does not silence a NaN: such elements of V become zeros here, and NaN goes to the
+      // columns that do see one.
+      bool nan = false;
+      static_for<8>([&](auto sc) __attribute__((always_inline)) {
+        constexpr int S = decltype(sc)::value, SH = 8 * (S % 4);
+        const bool in = S >= lo && S < hi, is_nan = ((r.vs[S / 4] >> SH) & 255u) == kScaleNaN;
+        nan |= in && is_nan;
+        if (!in || is_nan) {
+          r.vs[S / 4] = (r.vs[S / 4] & ~(255u << SH)) | 127u << SH;
+          constexpr int B0 = S * L::kLaneBytes;
+          if constexpr (L::kLaneBytes == 2) {
+            r.v[B0 / 4] &= B0 % 4 == 0 ? 0xffff0000u : 0x0000ffffu;
+          } else {
+#pragma unroll
+            for (int w = 0; w < L::kLaneBytes / 4; ++w) r.v[B0 / 4 + w] = 0u;
+          }
+        }
+      });
+      if (__any(nan)) {
+        const unsigned char* vs = block_ptr(blk) + L::kVScales + out_group * kPackRows;
+        for (int i = 0; i < kPackRows; ++i) {
+          const int64_t row = row0 + i;
+          if (vs[i] != kScaleNaN || row < seq.first) continue;
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            if (row <= last[n])
+#pragma unroll
+              for (int m = 0; m < MT; ++m) o[m][n] = f32x4{NAN, NAN, NAN, NAN};
+        }
+      }
+    }
+    // Online softmax.  The reference of the exponents follows the running maximum lazily: it moves when a score exceeds
+    // it by more than 2^8, so probabilities stay below 256 and rescaling is rare.
+    float mx[NT];
+    bool moves = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      mx[n] = m_limit[n];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx[n] = fmaxf(mx[n], s[u][n][i]);
+      mx[n] = reduce_rows_one(mx[n], [](float x, float y) { return fmaxf(x, y); });
+      moves |= mx[n] > m_limit[n];
+    }
+    if (__any(moves)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        if (mx[n] > m_limit[n]) {
+          const float m_new = mx[n] * a.scale_log2;
+          const float alpha = __builtin_amdgcn_exp2f(m_run[n] - m_new);   // (0 from the first reference on)
+          m_run[n] = m_new;
+          m_limit[n] = mx[n] + limit_step;
+          l_run[n] *= alpha;
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[m][n][i] *= alpha;
+        }
+    }
+    bf16x8 pf[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float m_use = m_run[n] == -INFINITY ? 0.f : m_run[n];
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][n][i % 4], a.scale_log2, -m_use));
+      l_run[n] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      // bf16 operands: half a step is 2^-9 of a probability, independent from key to key; the sum above is unrounded
+      const u32x4 w = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
+      pf[n] = __builtin_bit_cast(bf16x8, w);
+    }
+    // O^T += V^T P^T
+    float v_scale[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w = r.vs[i / 4];
+      v_scale[i] = __uint_as_float((i % 4 == 3 ? w >> 1 : w << (23 - 8 * (i % 4))) & 0x7f800000u);
+    }
+    static_for<MT / 2>([&](auto ec) __attribute__((always_inline)) {
+      constexpr int E2 = decltype(ec)::value;
+      uint32_t c[8];
+      static_for<8>([&](auto sc) __attribute__((always_inline)) {
+        constexpr int S = decltype(sc)::value;
+        c[S] = v_pair<D, BITS, S, E2>(r.v, v_scale[S]);
+      });
+      u32x4 even, odd;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        even[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x05040100u);
+        odd[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x07060302u);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        o[2 * E2][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pf[n], o[2 * E2][n], 0, 0, 0);
+        o[2 * E2 + 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pf[n], o[2 * E2 + 1][n], 0, 0, 0);
+      }
+    });
+  };
+
+  // ---- the blocks of this wave, the next one on its way while one is worked on ---------------------------------
+  int blk = blk0 + wave;
+  if (blk < blk1) {
+    R ra, rb;
+    load(ra, blk);
+    for (;;) {
+      const int b2 = blk + kWaves;
+      load(rb, min(b2, blk1 - 1));
+      compute(ra, blk);
+      if (b2 >= blk1) break;
+      blk = b2 + kWaves;
+      load(ra, min(blk, blk1 - 1));
+      compute(rb, b2);
+      if (blk >= blk1) break;
+    }
+  }
+
+  // ---- the four waves joined ---------------------------------------------------------------------------
+  __shared__ __align__(16) float o_lds[kWaves][16][D + 4];
+  __shared__ float m_lds[kWaves][16 * NT], l_lds[kWaves][16 * NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const float l_tot = reduce_rows_one(l_run[n], [](float x, float y) { return x + y; });
+    if (h == 0) {
+      m_lds[wave][16 * n + l16] = m_run[n];
+      l_lds[wave][16 * n + l16] = l_tot;
+    }
+  }
+  __syncthreads();
+  const bool final = seq.n_parts <= 1;
+  const int64_t item = ((int64_t)b * a.Hkv + g) * a.n_parts + part;
+  float* part_base = a.partial + item * n_cols * (D + 2);
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    auto top_of = [&](int c) __attribute__((always_inline)) {
+      float m = m_lds[0][c];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) m = fmaxf(m, m_lds[w][c]);
+      return m;
+    };
+    {
+      const float top = top_of(16 * n + l16);
+      const float f = m_run[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[n] - top);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int m = 0; m < MT; m += 4)
+          *reinterpret_cast<f32x4*>(&o_lds[wave][l16][(4 * h + i) * MT + m]) =
+              f32x4{o[m][n][i], o[m + 1][n][i], o[m + 2][n][i], o[m + 3][n][i]} * f;
+    }
+    __syncthreads();
+    constexpr int PER = D / 16;                        // 16 threads per column
+    const int c_l = threadIdx.x >> 4, c = 16 * n + c_l, d0 = (threadIdx.x & 15) * PER;
+    const int col = col0 + c;
+    if (col < n_cols) {
+      const float top = top_of(c);
+      float total = 0.f;
+      f32x4 acc[PER / 4];
+#pragma unroll
+      for (int e = 0; e < PER / 4; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float m = m_lds[w][c];
+        total += m == -INFINITY ? 0.f : l_lds[w][c] * __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+        for (int e = 0; e < PER / 4; ++e) acc[e] += *reinterpret_cast<const f32x4*>(&o_lds[w][c_l][d0 + 4 * e]);
+      }
+      if (final) {
+        const int t = col >> a.group_shift;
+        const int64_t row = ((int64_t)b * a.n_new + t) * a.Hq + g * G + (col & (G - 1));
+        const float inv = top == -INFINITY ? 0.f : 1.0f / total;
+        uint32_t w[PER / 2];
+#pragma unroll
+        for (int e = 0; e < PER / 2; ++e) w[e] = pack_bf16(acc[e / 2][e % 2 * 2] * inv, acc[e / 2][e % 2 * 2 + 1] * inv);
+        uint16_t* op = a.out + row * D + d0;
+        if constexpr (PER == 8) *reinterpret_cast<u32x4*>(op) = u32x4{w[0], w[1], w[2], w[3]};
+        else *reinterpret_cast<u32x2*>(op) = u32x2{w[0], w[1]};
+        if (a.lse != nullptr && d0 == 0)
+          a.lse[row] = top == -INFINITY ? -INFINITY : (top + __builtin_log2f(total)) * 0.69314718055994531f;
+      } else {
+#pragma unroll
+        for (int e = 0; e < PER / 4; ++e) *reinterpret_cast<f32x4*>(part_base + (int64_t)col * D + d0 + 4 * e) = acc[e];
+        if (d0 == 0) {
+          part_base[(int64_t)n_cols * D + col] = top;
+          part_base[(int64_t)n_cols * (D + 1) + col] = total;
+        }
+      }
+    }
+    if (n + 1 < NT) __syncthreads();
+  }
+}
+
+// The parts of a key range joined: out = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(m_i - max m).  One wave per query row.
+template <int D>
+__global__ __launch_bounds__(64) void packed_merge_kernel(PackedAttnArgs a) {
+  const int lane = threadIdx.x;
+  const int G = 1 << a.group_shift, n_cols = a.n_new << a.group_shift;
+  const int64_t row = blockIdx.x;                       // (sequence, new token, query head)
+  const int hq = (int)(row % a.Hq);
+  const int64_t bt = row / a.Hq;
+  const int t = (int)(bt % a.n_new), b = (int)(bt / a.n_new);
+  const int np = sequence_of(a, b).n_parts;
+  if (np <= 1) return;                                  // written by the attention kernel
+  const int g = hq >> a.group_shift, col = (t << a.group_shift) + (hq & (G - 1));
+  const int64_t stride = (int64_t)n_cols * (D + 2);
+  const float* base = a.partial + ((int64_t)b * a.Hkv + g) * a.n_parts * stride;
+  float top = -INFINITY;
+  for (int i = lane; i < np; i += 64) top = fmaxf(top, base[i * stride + (int64_t)n_cols * D + col]);
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+  constexpr int PER = D / 64;
+  float acc[PER] = {}, total = 0.f;
+  for (int i = 0; i < np; ++i) {
+    const float* p = base + i * stride;
+    const float m = p[(int64_t)n_cols * D + col];
+    if (m == -INFINITY) continue;
+    const float w = __builtin_amdgcn_exp2f(m - top);
+    total += w * p[(int64_t)n_cols * (D + 1) + col];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[e] += w * p[(int64_t)col * D + lane * PER + e];
+  }
+  const float inv = top == -INFINITY ? 0.f : 1.0f / total;
+  if constexpr (PER == 2) {
+    reinterpret_cast<uint32_t*>(a.out + row * D)[lane] = pack_bf16(acc[0] * inv, acc[1] * inv);
+  } else {
+    a.out[row * D + lane] = (uint16_t)pack_bf16(acc[0] * inv, 0.f);
+  }
+  if (a.lse != nullptr && lane == 0)
+    a.lse[row] = top == -INFINITY ? -INFINITY : (top + __builtin_log2f(total)) * 0.69314718055994531f;
+}
+
+struct PackedPlan {
+  int col_tiles;      // 16-column tiles per workgroup
+  int col_blocks;
+  int part_blocks;    // blocks of 32 rows per part
+  int n_parts;
+  size_t ws_bytes;
+};
+
+// The key range is divided until about four workgroups of four waves (what a compute unit holds) stand on each
+// compute unit, into parts of at least 256 rows (two blocks per wave).
+PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, int64_t max_len) {
+  PackedPlan p;
+  const int64_t n_cols = n_new * (cfg->n_q_heads / cfg->n_kv_heads);
+  p.col_tiles = n_cols > 16 ? 2 : 1;
+  p.col_blocks = (int)((n_cols + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
+  const int64_t blocks = (max_len + kPackRows - 1) / kPackRows + 1;   // a sequence may start inside a block
+  const int64_t groups = n_seq * cfg->n_kv_heads * p.col_blocks;
+  int64_t parts = (4 * kNumCUs + groups - 1) / groups;
+  int64_t per = (blocks + parts - 1) / parts;
+  if (per < 8) per = 8;
+  p.part_blocks = (int)per;
+  p.n_parts = (int)((blocks + per - 1) / per);
+  if (p.n_parts < 1) p.n_parts = 1;
+  p.ws_bytes = p.n_parts > 1 ? (size_t)(n_seq * cfg->n_kv_heads * p.n_parts) * n_cols * (cfg->head_dim + 2) * sizeof(float) : 0;
+  return p;
+}
+
+ct_status check_attn_sizes(const ct_layer_cfg* cfg, int32_t n_seq, int32_t n_new, int32_t max_len) {
+  if (n_seq < 0 || max_len < 0) return fail(CT_ERR_SHAPE, "negative size (n_seq %d, max_len %d)", n_seq, max_len);
+  if (n_new < 1) return fail(CT_ERR_SHAPE, "n_new %d must be at least 1", n_new);
+  if (n_new > 64) return fail(CT_ERR_UNSUPPORTED, "n_new %d: at most 64 new tokens per sequence", n_new);
+  if ((int64_t)n_seq * n_new * cfg->n_q_heads > 0x7fffffff)
+    return fail(CT_ERR_UNSUPPORTED, "n_seq %d x n_new %d x %d heads are too many rows for one launch", n_seq, n_new, cfg->n_q_heads);
+  return CT_OK;
+}
+
+}  // namespace
+
+}  // namespace ct
+
+using namespace ct;
+
+extern "C" {
+
+size_t ct_packed_attention_workspace_bytes(const ct_layer_cfg* cfg, int32_t n_seq, int32_t n_new, int32_t max_len) {
+  if (check_cfg(cfg) != CT_OK || check_attn_sizes(cfg, n_seq, n_new, max_len) != CT_OK || n_seq == 0) return 0;
+  return plan_packed(cfg, n_seq, n_new, max_len).ws_bytes;
+}
+
+ct_status ct_packed_attention(const ct_layer_cfg* cfg, const void* q, int32_t n_seq, int32_t n_new, const void* cache,
+                              int32_t n_rows, int32_t bits, const int32_t* seq_start, const int32_t* seq_len, int32_t max_len,
+                              void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  ct_status st = check_packed(cfg, n_rows, bits);
+  if (st != CT_OK) return st;
+  if ((st = check_attn_sizes(cfg, n_seq, n_new, max_len)) != CT_OK) return st;
+  if (max_len > n_rows) return fail(CT_ERR_SHAPE, "max_len %d exceeds the cache's %d rows", max_len, n_rows);
+  if (n_seq == 0) return CT_OK;
+  if (!q || !cache || !seq_start || !seq_len || !out)
+    return fail(CT_ERR_NULL, "q, cache, seq_start, seq_len and out must be non-NULL");
+  if ((((uintptr_t)q | (uintptr_t)cache | (uintptr_t)out) & 15) != 0)
+    return fail(CT_ERR_UNSUPPORTED, "q, cache and out must be 16-byte aligned");
+  const PackedPlan p = plan_packed(cfg, n_seq, n_new, max_len);
+  const int64_t groups = (int64_t)n_seq * cfg->n_kv_heads * p.col_blocks * p.n_parts;
+  if (groups > 0x7fffffff) return fail(CT_ERR_UNSUPPORTED, "n_seq %d with max_len %d: too many workgroups", n_seq, max_len);
+  if (p.ws_bytes > 0) {
+    if (workspace == nullptr) return fail(CT_ERR_WORKSPACE, "workspace is NULL but %zu bytes are needed", p.ws_bytes);
+    if (workspace_bytes < p.ws_bytes)
+      return fail(CT_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, p.ws_bytes);
+    if (((uintptr_t)workspace & 255) != 0) return fail(CT_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+  }
+  PackedAttnArgs a;
+  a.q = static_cast<const uint16_t*>(q);
+  a.cache = static_cast<const unsigned char*>(cache);
+  a.seq_start = seq_start;
+  a.seq_len = seq_len;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.partial = static_cast<float*>(workspace);
+  a.n_seq = n_seq;
+  a.n_new = n_new;
+  a.n_rows = n_rows;
+  a.max_len = max_len;
+  a.Hq = cfg->n_q_heads;
+  a.Hkv = cfg->n_kv_heads;
+  a.group_shift = 0;
+  while ((a.Hkv << a.group_shift) < a.Hq) ++a.group_shift;
+  a.n_parts = p.n_parts;
+  a.part_blocks = p.part_blocks;
+  a.col_blocks = p.col_blocks;
+  const float scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / sqrtf((float)cfg->head_dim);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto launch = [&](auto kernel) {
+    launch_kernel(KC_PACKED_ATTN, kernel, dim3((unsigned)groups), dim3(64 * kWaves), 0, s, a);
+  };
+  auto by_cols = [&](auto one, auto two) { p.col_tiles == 1 ? launch(one) : launch(two); };
+  if (cfg->head_dim == 128)
+    bits == 4 ? by_cols(packed_attn_kernel<128, 4, 1>, packed_attn_kernel<128, 4, 2>)
+              : by_cols(packed_attn_kernel<128, 8, 1>, packed_attn_kernel<128, 8, 2>);
+  else
+    bits == 4 ? by_cols(packed_attn_kernel<64, 4, 1>, packed_attn_kernel<64, 4, 2>)
+              : by_cols(packed_attn_kernel<64, 8, 1>, packed_attn_kernel<64, 8, 2>);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(e, "packed attention kernel launch");
+  if (p.n_parts > 1) {
+    const dim3 grid((unsigned)((int64_t)n_seq * n_new * cfg->n_q_heads));
+    if (cfg->head_dim == 128) launch_kernel(KC_MERGE, packed_merge_kernel<128>, grid, dim3(64), 0, s, a);
+    else launch_kernel(KC_MERGE, packed_merge_kernel<64>, grid, dim3(64), 0, s, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "packed attention merge kernel launch");
+  }
+  return CT_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,40 @@
+// Rotation of 8 pairs held in fp32, rounded to bf16 once: shared by the read-back of packed keys and the norm of
+// queries and keys.
+#pragma once
+
+#include "ct_internal.h"
+
+namespace ct {
+
+// Element offsets, inside a head row, of the two 16-byte pieces of the thread that owns pairs 8 jg .. 8 jg + 7.
+template <int D, int STYLE>
+__device__ __forceinline__ int piece_a(int jg) { return STYLE == 0 ? jg * 8 : jg * 16; }
+template <int D, int STYLE>
+__device__ __forceinline__ int piece_b(int jg) { return STYLE == 0 ? jg * 8 + D / 2 : jg * 16 + 8; }
+
+__device__ __forceinline__ void widen8(u32x4 x, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = bf16_lo(x[i]);
+    f[2 * i + 1] = bf16_hi(x[i]);
+  }
+}
+
+// STYLE 0: pair i is element i of `a` and of `b`; STYLE 1: elements 2i and 2i + 1 of the 16 in `a`, then `b`.
+template <int STYLE>
+__device__ __forceinline__ void rotate8(const float (&a)[8], const float (&b)[8], const float (&cs)[8], const float (&sn)[8],
+                                        u32x4& ra, u32x4& rb) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = 2 * i, f = 2 * i + 1;
+    if (STYLE == 0) {
+      ra[i] = pack_bf16(a[e] * cs[e] - b[e] * sn[e], a[f] * cs[f] - b[f] * sn[f]);
+      rb[i] = pack_bf16(a[e] * sn[e] + b[e] * cs[e], a[f] * sn[f] + b[f] * cs[f]);
+    } else {
+      ra[i] = pack_bf16(a[e] * cs[i] - a[f] * sn[i], a[e] * sn[i] + a[f] * cs[i]);
+      rb[i] = pack_bf16(b[e] * cs[4 + i] - b[f] * sn[4 + i], b[e] * sn[4 + i] + b[f] * cs[4 + i]);
+    }
+  }
+}
+
+}  // namespace ct
