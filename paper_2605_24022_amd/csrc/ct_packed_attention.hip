@@ -20,6 +20,7 @@ namespace ct {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int kMaxParts = 2 * kNumCUs;
 
 struct PackedAttnArgs {
   const uint16_t* q;              // [n_seq, n_new, Hq, D]
@@ -28,7 +29,8 @@ struct PackedAttnArgs {
   const int32_t* seq_len;
   uint16_t* out;
   float* lse;
-  float* partial;                 // per (sequence, KV head, part): O [C][D], then m [C], l [C]
+  float* partial;                 // O of every part: [sequence, KV head][part][column][D]
+  float* partial_ml;              // and its (m, l): [sequence, KV head][column][part]
   int32_t n_seq, n_new, n_rows, max_len;
   int32_t Hq, Hkv, group_shift;   // query heads per KV head: 1 << group_shift
   int32_t n_parts, part_blocks;   // parts of the key range, and blocks of 32 rows in each
@@ -39,18 +41,18 @@ struct PackedAttnArgs {
 // The rows of sequence b in the cache, and the parts its blocks are divided into.  Lengths and starts that do not
 // fit the cache are cut to it.
 struct Sequence {
-  int64_t first, end;   // rows [first, end)
+  int32_t first, end;   // rows [first, end)
   int32_t b0, b1;       // blocks [b0, b1)
   int32_t n_parts;
 };
 __device__ __forceinline__ Sequence sequence_of(const PackedAttnArgs& a, int b) {
   Sequence s;
-  const int64_t start = a.seq_start[b], len = min(a.seq_len[b], a.max_len);
-  s.first = start;
-  s.end = min(start + len, (int64_t)a.n_rows);
-  if (start < 0 || s.end <= start) s.first = s.end = 0;
-  s.b0 = (int32_t)(s.first / kPackRows);
-  s.b1 = (int32_t)((s.end + kPackRows - 1) / kPackRows);
+  const int32_t start = a.seq_start[b], len = min(a.seq_len[b], a.max_len);
+  const bool some = start >= 0 && start < a.n_rows && len > 0;
+  s.first = some ? start : 0;
+  s.end = some ? start + min(len, a.n_rows - start) : 0;
+  s.b0 = s.first / kPackRows;
+  s.b1 = (s.end + kPackRows - 1) / kPackRows;
   s.n_parts = (s.b1 - s.b0 + a.part_blocks - 1) / a.part_blocks;
   return s;
 }
@@ -108,7 +110,9 @@ __device__ __forceinline__ uint32_t v_pair(const uint32_t* v, float scale) {
 }
 
 template <int D, int BITS, int NT>
-__global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(PackedAttnArgs a) {
+// Registers for three waves per SIMD (16 columns) or two (32): left alone the compiler keeps the accumulators in
+// registers of their own and two waves, or one, remain.
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT == 1 ? 3 : 2))) void packed_attn_kernel(PackedAttnArgs a) {
   using L = PackLayout<D, BITS>;
   using R = Raw<D, BITS>;
   constexpr int KS = D / 32;
@@ -131,7 +135,7 @@ __global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(PackedAttnArgs
   const int n_cols = a.n_new << a.group_shift;
   const int col0 = cb * 16 * NT;
   bf16x8 qf[NT][KS];
-  int64_t last[NT];                                   // the last row that the column sees
+  int32_t last[NT];                                   // the last row that the column sees
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int c = min(col0 + 16 * n + l16, n_cols - 1);
@@ -141,7 +145,7 @@ __global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(PackedAttnArgs
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[n][ks] = *reinterpret_cast<const bf16x8*>(qp + 8 * ks);
   }
-  const int64_t first_last = seq.end - a.n_new + (col0 >> a.group_shift);   // the lowest of `last`
+  const int32_t first_last = seq.end - a.n_new + (col0 >> a.group_shift);   // the lowest of `last`
 
   // ---- where a lane finds its share of a block -------------------------------------------------------
   const int k_row = 8 * (l16 >> 2) + (l16 & 3);       // row of 16-key tile 0; tile 1: 4 rows further on
@@ -192,13 +196,12 @@ __global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(PackedAttnArgs
       }
     // Blocks that reach over an end of the sequence, or past the earliest of the new tokens: rows outside the
     // sequence may hold anything, rows that only some columns see may hold NaN.
-    const int64_t row0 = (int64_t)blk * kPackRows;
+    const int32_t row0 = blk * kPackRows;
     if (row0 < seq.first || row0 + kPackRows - 1 > first_last) {
-      const int lo = (int)max(seq.first - row0 - 8 * h, (int64_t)0);         // keys [lo, hi) of the lane's eight are rows
-      const int hi = (int)min(seq.end - row0 - 8 * h, (int64_t)8);           // of the sequence
+      const int lo = seq.first - row0 - 8 * h, hi = seq.end - row0 - 8 * h;   // keys [lo, hi) of the lane's eight are the sequence's
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const int rel = (int)min(last[n] - row0 - 8 * h, (int64_t)8);
+        const int rel = last[n] - row0 - 8 * h;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -225,15 +228,18 @@ __global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(PackedAttnArgs
       });
       if (__any(nan)) {
         const unsigned char* vs = block_ptr(blk) + L::kVScales + out_group * kPackRows;
+        bool sees[NT] = {};
+#pragma unroll 1
         for (int i = 0; i < kPackRows; ++i) {
-          const int64_t row = row0 + i;
-          if (vs[i] != kScaleNaN || row < seq.first) continue;
+          const int32_t row = row0 + i;
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-            if (row <= last[n])
-#pragma unroll
-              for (int m = 0; m < MT; ++m) o[m][n] = f32x4{NAN, NAN, NAN, NAN};
+          for (int n = 0; n < NT; ++n) sees[n] |= vs[i] == kScaleNaN && row >= seq.first && row <= last[n];
         }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          if (sees[n])
+#pragma unroll
+            for (int m = 0; m < MT; ++m) o[m][n] = f32x4{NAN, NAN, NAN, NAN};
       }
     }
     // Online softmax.  The reference of the exponents follows the running maximum lazily: it moves when a score exceeds
@@ -306,19 +312,18 @@ __global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(PackedAttnArgs
   };
 
   // ---- the blocks of this wave, the next one on its way while one is worked on ---------------------------------
-  int blk = blk0 + wave;
-  if (blk < blk1) {
-    R ra, rb;
-    load(ra, blk);
-    for (;;) {
-      const int b2 = blk + kWaves;
-      load(rb, min(b2, blk1 - 1));
-      compute(ra, blk);
-      if (b2 >= blk1) break;
-      blk = b2 + kWaves;
-      load(ra, min(blk, blk1 - 1));
-      compute(rb, b2);
-      if (blk >= blk1) break;
+  // (Two or three blocks ahead instead of one: within 3 % of this with 4-bit codes, registers spill with 8-bit ones.)
+  if (blk0 + wave < blk1) {
+    R r[2];
+    load(r[0], blk0 + wave);
+    for (int blk = blk0 + wave; blk < blk1;) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        load(r[1 - i], min(blk + kWaves, blk1 - 1));
+        compute(r[i], blk);
+        blk += kWaves;
+        if (blk >= blk1) break;
+      }
     }
   }
 
@@ -335,8 +340,7 @@ __global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(PackedAttnArgs
   }
   __syncthreads();
   const bool final = seq.n_parts <= 1;
-  const int64_t item = ((int64_t)b * a.Hkv + g) * a.n_parts + part;
-  float* part_base = a.partial + item * n_cols * (D + 2);
+  const int64_t pair = (int64_t)b * a.Hkv + g;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     auto top_of = [&](int c) __attribute__((always_inline)) {
@@ -385,22 +389,24 @@ __global__ __launch_bounds__(64 * kWaves) void packed_attn_kernel(PackedAttnArgs
         if (a.lse != nullptr && d0 == 0)
           a.lse[row] = top == -INFINITY ? -INFINITY : (top + __builtin_log2f(total)) * 0.69314718055994531f;
       } else {
+        float* op = a.partial + ((pair * a.n_parts + part) * n_cols + col) * D + d0;
 #pragma unroll
-        for (int e = 0; e < PER / 4; ++e) *reinterpret_cast<f32x4*>(part_base + (int64_t)col * D + d0 + 4 * e) = acc[e];
-        if (d0 == 0) {
-          part_base[(int64_t)n_cols * D + col] = top;
-          part_base[(int64_t)n_cols * (D + 1) + col] = total;
-        }
+        for (int e = 0; e < PER / 4; ++e) *reinterpret_cast<f32x4*>(op + 4 * e) = acc[e];
+        if (d0 == 0) reinterpret_cast<f32x2*>(a.partial_ml)[(pair * n_cols + col) * a.n_parts + part] = f32x2{top, total};
       }
     }
     if (n + 1 < NT) __syncthreads();
   }
 }
 
-// The parts of a key range joined: out = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(m_i - max m).  One wave per query row.
+// The parts of a key range joined: out = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(m_i - max m).  One workgroup per query
+// row: the weights first, a thread each, then D / 4 threads side by side over a part's row and 1024 / D parts at a time.
+// (One wave per row and one part after the other took 44 us for 32 rows of 128 parts.)
+constexpr int kMergeThreads = 256;
 template <int D>
-__global__ __launch_bounds__(64) void packed_merge_kernel(PackedAttnArgs a) {
-  const int lane = threadIdx.x;
+__global__ __launch_bounds__(kMergeThreads) void packed_merge_kernel(PackedAttnArgs a) {
+  constexpr int LANES = D / 4, SLOTS = kMergeThreads / LANES;
+  const int tid = threadIdx.x;
   const int G = 1 << a.group_shift, n_cols = a.n_new << a.group_shift;
   const int64_t row = blockIdx.x;                       // (sequence, new token, query head)
   const int hq = (int)(row % a.Hq);
@@ -408,31 +414,46 @@ __global__ __launch_bounds__(64) void packed_merge_kernel(PackedAttnArgs a) {
   const int t = (int)(bt % a.n_new), b = (int)(bt / a.n_new);
   const int np = sequence_of(a, b).n_parts;
   if (np <= 1) return;                                  // written by the attention kernel
-  const int g = hq >> a.group_shift, col = (t << a.group_shift) + (hq & (G - 1));
-  const int64_t stride = (int64_t)n_cols * (D + 2);
-  const float* base = a.partial + ((int64_t)b * a.Hkv + g) * a.n_parts * stride;
+  const int col = (t << a.group_shift) + (hq & (G - 1));
+  const int64_t pair = (int64_t)b * a.Hkv + (hq >> a.group_shift);
+  const f32x2* ml = reinterpret_cast<const f32x2*>(a.partial_ml) + (pair * n_cols + col) * a.n_parts;
+  __shared__ float w_lds[kMaxParts], red[kMergeThreads / 64], red_l[kMergeThreads / 64];
+  __shared__ __align__(16) float o_lds[SLOTS][D];
   float top = -INFINITY;
-  for (int i = lane; i < np; i += 64) top = fmaxf(top, base[i * stride + (int64_t)n_cols * D + col]);
+  for (int i = tid; i < np; i += kMergeThreads) top = fmaxf(top, ml[i][0]);
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-  constexpr int PER = D / 64;
-  float acc[PER] = {}, total = 0.f;
-  for (int i = 0; i < np; ++i) {
-    const float* p = base + i * stride;
-    const float m = p[(int64_t)n_cols * D + col];
-    if (m == -INFINITY) continue;
-    const float w = __builtin_amdgcn_exp2f(m - top);
-    total += w * p[(int64_t)n_cols * (D + 1) + col];
+  if ((tid & 63) == 0) red[tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  float total = 0.f;
+  for (int i = tid; i < np; i += kMergeThreads) {
+    const f32x2 x = ml[i];
+    const float w = x[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[0] - top);
+    w_lds[i] = w;
+    total += w * x[1];
+  }
 #pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] += w * p[(int64_t)col * D + lane * PER + e];
-  }
+  for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
+  if ((tid & 63) == 0) red_l[tid >> 6] = total;
+  __syncthreads();
+  total = (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
+  const int slot = tid / LANES, d0 = tid % LANES * 4;
+  const float* base = a.partial + (pair * a.n_parts * n_cols + col) * D + d0;
+  const int64_t stride = (int64_t)n_cols * D;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = slot; i < np; i += SLOTS) acc += w_lds[i] * *reinterpret_cast<const f32x4*>(base + i * stride);
+  *reinterpret_cast<f32x4*>(&o_lds[slot][d0]) = acc;
+  __syncthreads();
+  if (tid >= LANES) return;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i) sum += *reinterpret_cast<const f32x4*>(&o_lds[i][tid * 4]);
   const float inv = top == -INFINITY ? 0.f : 1.0f / total;
-  if constexpr (PER == 2) {
-    reinterpret_cast<uint32_t*>(a.out + row * D)[lane] = pack_bf16(acc[0] * inv, acc[1] * inv);
-  } else {
-    a.out[row * D + lane] = (uint16_t)pack_bf16(acc[0] * inv, 0.f);
-  }
-  if (a.lse != nullptr && lane == 0)
+  *reinterpret_cast<u32x2*>(a.out + row * D + tid * 4) =
+      u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
+  if (a.lse != nullptr && tid == 0)
     a.lse[row] = top == -INFINITY ? -INFINITY : (top + __builtin_log2f(total)) * 0.69314718055994531f;
 }
 
@@ -441,11 +462,18 @@ struct PackedPlan {
   int col_blocks;
   int part_blocks;    // blocks of 32 rows per part
   int n_parts;
-  size_t ws_bytes;
+  size_t o_bytes, ws_bytes;
 };
 
-// The key range is divided until about four workgroups of four waves (what a compute unit holds) stand on each
-// compute unit, into parts of at least 256 rows (two blocks per wave).
+// How the key range is divided.  One wave takes about 0.5 us for a block of 32 rows (260 vector instructions at 4
+// cycles each; 0.36 with heads of 64) and the launch of the merge costs 3 us: sequences of up to 1024 rows stay
+// whole (one token, 32/8 heads of 128, 1, 4 and 16 sequences of 1024 rows: 7.4, 7.7 and 7.8 us whole, 7.7, 8.7 and
+// 10.8 in parts; 8/2 heads of 64 5.7 and 7.8; one of 2048 rows 11.3 and 8.1, 8.6 and 7.7).
+// Longer ones are divided until two workgroups stand on each compute unit, into parts of at least 128 rows.  Targets of
+// 256 / 512 / 768 / 1024 / 2048 workgroups, 4 bits: 64 sequences of 4096 rows - / 51 / 58 / 58 / 60 us (5.6 TB/s with
+// 512), 1 of 32768 14.1 / 15.3 / 15.9 / 17.5 / 20.1, 8 of up to 16384 with four tokens 32.3 / 30.3 / 32.7 / 34.9 / 35.4,
+// 2 of 131072 in 8 bits 97.5 / 96.5 / 99.6 / 99.0 / 104: three fit a compute unit, and beyond them a second round
+// starts that does not fill.
 PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, int64_t max_len) {
   PackedPlan p;
   const int64_t n_cols = n_new * (cfg->n_q_heads / cfg->n_kv_heads);
@@ -453,13 +481,13 @@ PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, in
   p.col_blocks = (int)((n_cols + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
   const int64_t blocks = (max_len + kPackRows - 1) / kPackRows + 1;   // a sequence may start inside a block
   const int64_t groups = n_seq * cfg->n_kv_heads * p.col_blocks;
-  int64_t parts = (4 * kNumCUs + groups - 1) / groups;
+  int64_t parts = blocks * p.col_tiles <= 33 ? 1 : (2 * kNumCUs + groups - 1) / groups;
   int64_t per = (blocks + parts - 1) / parts;
-  if (per < 8) per = 8;
+  if (per < 4) per = 4;
   p.part_blocks = (int)per;
   p.n_parts = (int)((blocks + per - 1) / per);
-  if (p.n_parts < 1) p.n_parts = 1;
-  p.ws_bytes = p.n_parts > 1 ? (size_t)(n_seq * cfg->n_kv_heads * p.n_parts) * n_cols * (cfg->head_dim + 2) * sizeof(float) : 0;
+  p.o_bytes = (size_t)(n_seq * cfg->n_kv_heads * p.n_parts) * n_cols * cfg->head_dim * sizeof(float);
+  p.ws_bytes = p.n_parts > 1 ? p.o_bytes + p.o_bytes / cfg->head_dim * 2 : 0;
   return p;
 }
 
@@ -514,6 +542,7 @@ ct_status ct_packed_attention(const ct_layer_cfg* cfg, const void* q, int32_t n_
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
   a.partial = static_cast<float*>(workspace);
+  a.partial_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.o_bytes);
   a.n_seq = n_seq;
   a.n_new = n_new;
   a.n_rows = n_rows;
@@ -542,8 +571,8 @@ ct_status ct_packed_attention(const ct_layer_cfg* cfg, const void* q, int32_t n_
   if (e != hipSuccess) return hip_fail(e, "packed attention kernel launch");
   if (p.n_parts > 1) {
     const dim3 grid((unsigned)((int64_t)n_seq * n_new * cfg->n_q_heads));
-    if (cfg->head_dim == 128) launch_kernel(KC_MERGE, packed_merge_kernel<128>, grid, dim3(64), 0, s, a);
-    else launch_kernel(KC_MERGE, packed_merge_kernel<64>, grid, dim3(64), 0, s, a);
+    if (cfg->head_dim == 128) launch_kernel(KC_MERGE, packed_merge_kernel<128>, grid, dim3(kMergeThreads), 0, s, a);
+    else launch_kernel(KC_MERGE, packed_merge_kernel<64>, grid, dim3(kMergeThreads), 0, s, a);
     e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "packed attention merge kernel launch");
   }
