@@ -23,62 +23,78 @@ struct PackArgs {
   int32_t Hkv;
 };
 
-// One thread per 8 elements of a row of K or V (blockIdx.y), four neighbours share a scale.
+// A workgroup takes 32 tokens of one head (those of one block of the cache, where the rows are a run), so that every
+// line of the cache is written by one workgroup in whole: lines that several dies write in parts cost most of the
+// time.  A thread takes 8 elements at a time; threads lie along the row for K and along the tokens for V, which is the
+// order of their codes; the threads that share a scale are 1, 2 and 3 (K) or 8, 16 and 24 (V) apart.
 template <int D, int BITS>
 __global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
   using L = PackLayout<D, BITS>;
-  constexpr int PIECES = D / 8;
-  const int64_t gid = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int piece = (int)(gid % PIECES);
-  const int64_t rest = gid / PIECES;
-  const int head = (int)(rest % a.Hkv);
-  const int64_t t = rest / a.Hkv;
-  if (t >= a.n_tokens) return;
-  const int32_t row = a.rows != nullptr ? a.rows[t] : a.first_row + (int32_t)t;
-  if (row < 0 || row >= a.n_rows) return;   // (the same for the four lanes of a group)
-  const bool is_v = blockIdx.y != 0;
-  u32x4 x = *reinterpret_cast<const u32x4*>((is_v ? a.v + t * a.v_stride : a.k + t * a.k_stride) + head * D + piece * 8);
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = x[i] & 0x7fffu, hi = (x[i] >> 16) & 0x7fffu;
-    top = max(top, max(lo, hi));
-  }
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-  if (top > kMaxBits && top < 0x7f80u) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = clamp_pair(x[i]);
-    top = kMaxBits;
-  }
-  const uint32_t sb = scale_byte<BITS>(top);
-  // (a group that holds infinities or NaN reads back as NaN whatever its codes are: they are cleared)
-  u32x2 w = pack8<BITS>(x, scale_of(sb));
-  if (sb == kScaleNaN) w = u32x2{0u, 0u};
-  unsigned char* block = a.cache + ((int64_t)(row / kPackRows) * a.Hkv + head) * L::kBytes;
-  const int r = row % kPackRows, group = piece / 4;
-  if (!is_v) {
-    unsigned char* p = block + L::k_code(r, piece * 8);
-    if (BITS == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
-    else *reinterpret_cast<u32x2*>(p) = w;
-    if (piece % 4 == 0) block[L::k_scale(r, group)] = (unsigned char)sb;
-  } else {
-    unsigned char* p = block + L::v_code(r, piece * 8);
-    if (D == 128) {
-      if (BITS == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
-      else *reinterpret_cast<u32x2*>(p) = w;
-    } else {   // two lanes of the attention hold four of the elements each
-      unsigned char* p2 = block + L::v_code(r, piece * 8 + 4);
-      if (BITS == 4) {
-        *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
-        *reinterpret_cast<uint16_t*>(p2) = (uint16_t)(w[0] >> 16);
-      } else {
-        *reinterpret_cast<uint32_t*>(p) = w[0];
-        *reinterpret_cast<uint32_t*>(p2) = w[1];
-      }
+  constexpr int PIECES = D / 8, STEP = kThreads / PIECES;      // pieces of a row, rows per step
+  const int head = blockIdx.x % a.Hkv;
+  const int skip = a.rows != nullptr ? 0 : a.first_row % kPackRows;      // rows of the first block ahead of the run
+  const int64_t t0 = (int64_t)(blockIdx.x / a.Hkv) * kPackRows - skip;
+  const int tid = threadIdx.x;
+  u32x4 x[2][kPackRows / STEP];
+  int32_t row[2][kPackRows / STEP];
+  auto place = [&](bool is_v, int i, int& tok, int& piece) __attribute__((always_inline)) {
+    if (is_v) {
+      tok = i * STEP + (tid / (8 * PIECES)) * 8 + tid % 8;
+      piece = tid / 8 % PIECES;
+    } else {
+      tok = i * STEP + tid / PIECES;
+      piece = tid % PIECES;
     }
-    if (piece % 4 == 0) block[L::v_scale(r, group)] = (unsigned char)sb;
-  }
+  };
+#pragma unroll
+  for (int v = 0; v < 2; ++v)
+#pragma unroll
+    for (int i = 0; i < kPackRows / STEP; ++i) {
+      int tok, piece;
+      place(v != 0, i, tok, piece);
+      const int64_t t = t0 + tok;
+      row[v][i] = t < 0 || t >= a.n_tokens ? -1 : a.rows != nullptr ? a.rows[t] : a.first_row + (int32_t)t;
+      if (row[v][i] >= 0) x[v][i] = *reinterpret_cast<const u32x4*>((v ? a.v + t * a.v_stride : a.k + t * a.k_stride) + head * D + piece * 8);
+    }
+#pragma unroll
+  for (int v = 0; v < 2; ++v)
+#pragma unroll
+    for (int i = 0; i < kPackRows / STEP; ++i) {
+      if (row[v][i] < 0 || row[v][i] >= a.n_rows) continue;     // (the same for the four threads of a scale)
+      int tok, piece;
+      place(v != 0, i, tok, piece);
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = max(top, max(x[v][i][e] & 0x7fffu, (x[v][i][e] >> 16) & 0x7fffu));
+      top = max(top, (uint32_t)__shfl_xor((int)top, v ? 8 : 1));
+      top = max(top, (uint32_t)__shfl_xor((int)top, v ? 16 : 2));
+      if (top > kMaxBits && top < 0x7f80u) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[v][i][e] = clamp_pair(x[v][i][e]);
+        top = kMaxBits;
+      }
+      const uint32_t sb = scale_byte<BITS>(top);
+      // (a group that holds infinities or NaN reads back as NaN whatever its codes are: they are cleared)
+      u32x2 w = pack8<BITS>(x[v][i], scale_of(sb));
+      if (sb == kScaleNaN) w = u32x2{0u, 0u};
+      unsigned char* block = a.cache + ((int64_t)(row[v][i] / kPackRows) * a.Hkv + head) * L::kBytes;
+      const int r = row[v][i] % kPackRows, group = piece / 4;
+      unsigned char* p = block + (v ? L::v_code(r, piece * 8) : L::k_code(r, piece * 8));
+      if (v == 0 || D == 128) {
+        if (BITS == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+        else *reinterpret_cast<u32x2*>(p) = w;
+      } else {   // two lanes of the attention hold four of the elements each
+        unsigned char* p2 = block + L::v_code(r, piece * 8 + 4);
+        if (BITS == 4) {
+          *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+          *reinterpret_cast<uint16_t*>(p2) = (uint16_t)(w[0] >> 16);
+        } else {
+          *reinterpret_cast<uint32_t*>(p) = w[0];
+          *reinterpret_cast<uint32_t*>(p2) = w[1];
+        }
+      }
+      if (piece % 4 == 0) block[v ? L::v_scale(r, group) : L::k_scale(r, group)] = (unsigned char)sb;
+    }
 }
 
 struct UnpackArgs {
@@ -94,69 +110,122 @@ struct UnpackArgs {
   uint16_t* v;
 };
 
+// Codes and scale byte of eight elements, as they lie in the cache.
 template <int D, int BITS>
-__device__ __forceinline__ u32x4 load_k8(const unsigned char* block, int r, int dim) {
-  using L = PackLayout<D, BITS>;
-  const float scale = scale_of(block[L::k_scale(r, dim / kPackGroup)]);
-  const uint32_t* p = reinterpret_cast<const uint32_t*>(block + L::k_code(r, dim));
-  uint32_t w[2] = {p[0], BITS == 8 ? p[1] : 0u};
-  return unpack8<BITS>(w, scale);
-}
-template <int D, int BITS>
-__device__ __forceinline__ u32x4 load_v8(const unsigned char* block, int r, int dim) {
-  using L = PackLayout<D, BITS>;
-  const float scale = scale_of(block[L::v_scale(r, dim / kPackGroup)]);
-  const unsigned char* p = block + L::v_code(r, dim);
-  uint32_t w[2] = {0u, 0u};
-  if (D == 128) {
-    w[0] = reinterpret_cast<const uint32_t*>(p)[0];
-    if (BITS == 8) w[1] = reinterpret_cast<const uint32_t*>(p)[1];
-  } else {
-    const unsigned char* p2 = block + L::v_code(r, dim + 4);
-    if (BITS == 4) {
-      w[0] = *reinterpret_cast<const uint16_t*>(p) | (uint32_t) * reinterpret_cast<const uint16_t*>(p2) << 16;
-    } else {
+struct Packed8 {
+  uint32_t w[2];
+  uint32_t scale;
+  __device__ __forceinline__ void load_k(const unsigned char* block, int r, int dim) {
+    using L = PackLayout<D, BITS>;
+    const unsigned char* p = block + L::k_code(r, dim);
+    if constexpr (BITS == 4) {
       w[0] = *reinterpret_cast<const uint32_t*>(p);
-      w[1] = *reinterpret_cast<const uint32_t*>(p2);
+    } else {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+      w[0] = x[0];
+      w[1] = x[1];
     }
+    scale = block[L::k_scale(r, dim / kPackGroup)];
   }
-  return unpack8<BITS>(w, scale);
-}
+  __device__ __forceinline__ void load_v(const unsigned char* block, int r, int dim) {
+    using L = PackLayout<D, BITS>;
+    const unsigned char* p = block + L::v_code(r, dim);
+    if constexpr (D == 64) {      // two lanes of the attention hold four of the elements each
+      const unsigned char* p2 = block + L::v_code(r, dim + 4);
+      if constexpr (BITS == 4) {
+        w[0] = *reinterpret_cast<const uint16_t*>(p) | (uint32_t) * reinterpret_cast<const uint16_t*>(p2) << 16;
+      } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+        w[1] = *reinterpret_cast<const uint32_t*>(p2);
+      }
+    } else if constexpr (BITS == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+      w[0] = x[0];
+      w[1] = x[1];
+    }
+    scale = block[L::v_scale(r, dim / kPackGroup)];
+  }
+  __device__ __forceinline__ u32x4 value() const { return unpack8<BITS>(w, scale_of(scale)); }
+};
 
-// One thread per 8 rotation pairs of a token's head: cos and sin once per thread and head.
+// A workgroup takes a tile of tokens (32, or 64 with heads of 64) and two heads.  K: a thread owns 8 rotation pairs of one
+// token, its sines and cosines serve both heads.  V: a thread takes 8 elements, threads along the tokens, the order of
+// the codes; both write whole lines.  One, two, four or eight heads per workgroup: 8192 tokens in 4 bits 9.5 / 8.0 / 8.2 /
+// 10.3 us, 31901 in 8 bits 37 / 33.9 / 36.2 / 37.1.
+// The stores do not stay in the caches: 8.0 against 9.7 us and 33.9 against 42.1 (5.0 TB/s), and what follows in a partial
+// prefill takes as long as the call wins or loses by it (unpack, projection, scatter and attention of 15 % of 31901 rows
+// 1281 us with either, of 5 % 500 against 497; of 8192 186.6 against 186.0).
+constexpr int kUnpackHeads = 2;
 template <int D, int BITS, int STYLE>
 __global__ __launch_bounds__(kThreads) void unpack_kernel(UnpackArgs a, RopeTable table) {
   using L = PackLayout<D, BITS>;
-  constexpr int THREADS = D / 16;
-  const int64_t gid = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int jg = (int)(gid % THREADS);
-  const int64_t rest = gid / THREADS;
-  const int head = (int)(rest % a.Hkv);
-  const int64_t t = rest / a.Hkv;
-  if (t >= a.n_tokens) return;
-  const int32_t row = a.rows != nullptr ? a.rows[t] : a.first_row + (int32_t)t;
-  if (row < 0 || row >= a.n_rows) return;
-  const unsigned char* block = a.cache + ((int64_t)(row / kPackRows) * a.Hkv + head) * L::kBytes;
-  const int r = row % kPackRows;
-  const int d_a = piece_a<D, STYLE>(jg), d_b = piece_b<D, STYLE>(jg);
-  u32x4 ka = load_k8<D, BITS>(block, r, d_a), kb = load_k8<D, BITS>(block, r, d_b);
-  const u32x4 va = load_v8<D, BITS>(block, r, d_a), vb = load_v8<D, BITS>(block, r, d_b);
-  if (a.new_pos != nullptr) {
-    const int32_t delta = a.new_pos[t] - (a.old_pos != nullptr ? a.old_pos[t] : 0);
-    float cs[8], sn[8];
+  constexpr int PER_TOKEN = D / 16, TILE = kThreads / PER_TOKEN, PIECES = D / 8, STEP = kThreads / PIECES;
+  const int tid = threadIdx.x;
+  const int64_t t0 = (int64_t)blockIdx.x * TILE;
+  const int head0 = blockIdx.y * kUnpackHeads;
+  auto row_of = [&](int64_t t) __attribute__((always_inline)) {
+    int32_t row = -1;
+    if (t < a.n_tokens) row = a.rows != nullptr ? a.rows[t] : a.first_row + (int32_t)t;
+    return row < a.n_rows ? row : -1;
+  };
+  const int64_t t_k = t0 + tid / PER_TOKEN;
+  const int jg = tid % PER_TOKEN;
+  const int32_t row_k = row_of(t_k);
+  int32_t row_v[2];
+  int64_t t_v[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    t_v[i] = t0 + i * STEP + tid / (8 * PIECES) * 8 + tid % 8;
+    row_v[i] = row_of(t_v[i]);
+  }
+  const int d_a = piece_a<D, STYLE>(jg), d_b = piece_b<D, STYLE>(jg), d_v = tid / 8 % PIECES * 8;
+  // both heads are on their way while the angles are worked out
+  struct Head {
+    Packed8<D, BITS> ka, kb, v[2];
+  };
+  auto load = [&](Head& x, int head) __attribute__((always_inline)) {
+    if (row_k >= 0) {
+      const unsigned char* block = a.cache + ((int64_t)(row_k / kPackRows) * a.Hkv + head) * L::kBytes;
+      x.ka.load_k(block, row_k % kPackRows, d_a);
+      x.kb.load_k(block, row_k % kPackRows, d_b);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (row_v[i] >= 0) x.v[i].load_v(a.cache + ((int64_t)(row_v[i] / kPackRows) * a.Hkv + head) * L::kBytes, row_v[i] % kPackRows, d_v);
+  };
+  Head x[kUnpackHeads];
+#pragma unroll
+  for (int i = 0; i < kUnpackHeads; ++i)
+    if (head0 + i < a.Hkv) load(x[i], head0 + i);
+  const bool turns = a.new_pos != nullptr;
+  float cs[8], sn[8];
+  if (turns && row_k >= 0) {
+    const int32_t delta = a.new_pos[t_k] - (a.old_pos != nullptr ? a.old_pos[t_k] : 0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) sincos_turns(delta, table.turns[jg * 8 + i], cs[i], sn[i]);
-    float fa[8], fb[8];
-    widen8(ka, fa);
-    widen8(kb, fb);
-    rotate8<STYLE>(fa, fb, cs, sn, ka, kb);
   }
-  uint16_t* kd = a.k + (t * a.Hkv + head) * D;
-  uint16_t* vd = a.v + (t * a.Hkv + head) * D;
-  *reinterpret_cast<u32x4*>(kd + d_a) = ka;
-  *reinterpret_cast<u32x4*>(kd + d_b) = kb;
-  *reinterpret_cast<u32x4*>(vd + d_a) = va;
-  *reinterpret_cast<u32x4*>(vd + d_b) = vb;
+  auto finish = [&](const Head& x, int head) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (row_v[i] >= 0) __builtin_nontemporal_store(x.v[i].value(), reinterpret_cast<u32x4*>(a.v + (t_v[i] * a.Hkv + head) * D + d_v));
+    if (row_k >= 0) {
+      u32x4 ka = x.ka.value(), kb = x.kb.value();
+      if (turns) {
+        float fa[8], fb[8];
+        widen8(ka, fa);
+        widen8(kb, fb);
+        rotate8<STYLE>(fa, fb, cs, sn, ka, kb);
+      }
+      uint16_t* kd = a.k + (t_k * a.Hkv + head) * D;
+      __builtin_nontemporal_store(ka, reinterpret_cast<u32x4*>(kd + d_a));
+      __builtin_nontemporal_store(kb, reinterpret_cast<u32x4*>(kd + d_b));
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kUnpackHeads; ++i)
+    if (head0 + i < a.Hkv) finish(x[i], head0 + i);
 }
 
 }  // namespace
@@ -176,13 +245,6 @@ ct_status check_rows(const int32_t* rows, int32_t first_row, int32_t n_tokens, i
   if (rows == nullptr && (first_row < 0 || (int64_t)first_row + n_tokens > n_rows))
     return fail(CT_ERR_INDEX, "rows %d to %lld do not lie in the cache's %d", first_row, (long long)first_row + n_tokens - 1, n_rows);
   return CT_OK;
-}
-
-// Workgroups of kThreads for n_tokens x Hkv x per_head threads; false where the grid would not hold them.
-bool grid_for(int64_t n_tokens, int64_t Hkv, int64_t per_head, unsigned* blocks) {
-  const int64_t b = (n_tokens * Hkv * per_head + kThreads - 1) / kThreads;
-  *blocks = (unsigned)b;
-  return b <= 0x7fffffff;
 }
 
 }  // namespace
@@ -215,11 +277,12 @@ ct_status ct_pack_kv(const ct_layer_cfg* cfg, const void* k, int64_t k_stride, c
     return fail(CT_ERR_UNSUPPORTED, "k, v and cache must be 16-byte aligned and the strides multiples of 8");
   PackArgs a = {static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), k_stride, v_stride, rows, first_row, n_tokens,
                 static_cast<unsigned char*>(cache), n_rows, cfg->n_kv_heads};
-  unsigned blocks;
-  if (!grid_for(n_tokens, cfg->n_kv_heads, cfg->head_dim / 8, &blocks))
+  const int64_t tiles = ((rows != nullptr ? 0 : first_row % kPackRows) + (int64_t)n_tokens + kPackRows - 1) / kPackRows;
+  if (tiles * cfg->n_kv_heads > 0x7fffffff)
     return fail(CT_ERR_UNSUPPORTED, "n_tokens %d x %d heads are too many for one launch", n_tokens, cfg->n_kv_heads);
+  const dim3 grid((unsigned)(tiles * cfg->n_kv_heads));
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto launch = [&](auto kernel) { launch_kernel(KC_PACK, kernel, dim3(blocks, 2), dim3(kThreads), 0, s, a); };
+  auto launch = [&](auto kernel) { launch_kernel(KC_PACK, kernel, grid, dim3(kThreads), 0, s, a); };
   if (cfg->head_dim == 128) bits == 4 ? launch(pack_kernel<128, 4>) : launch(pack_kernel<128, 8>);
   else bits == 4 ? launch(pack_kernel<64, 4>) : launch(pack_kernel<64, 8>);
   hipError_t e = hipGetLastError();
@@ -241,13 +304,13 @@ ct_status ct_unpack_kv(const ct_layer_cfg* cfg, const void* cache, int32_t n_row
     return fail(CT_ERR_UNSUPPORTED, "cache, k_dst and v_dst must be 16-byte aligned");
   UnpackArgs a = {static_cast<const unsigned char*>(cache), n_rows, cfg->n_kv_heads, rows, first_row, old_pos, new_pos, n_tokens,
                   static_cast<uint16_t*>(k_dst), static_cast<uint16_t*>(v_dst)};
-  unsigned blocks;
-  if (!grid_for(n_tokens, cfg->n_kv_heads, cfg->head_dim / 16, &blocks))
-    return fail(CT_ERR_UNSUPPORTED, "n_tokens %d x %d heads are too many for one launch", n_tokens, cfg->n_kv_heads);
+  const int tile = kThreads / (cfg->head_dim / 16);
+  const unsigned tiles = (unsigned)(((int64_t)n_tokens + tile - 1) / tile);
+  const dim3 grid(tiles, (unsigned)((cfg->n_kv_heads + kUnpackHeads - 1) / kUnpackHeads));
   RopeTable table;
   fill_rope_table(cfg, &table);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto launch = [&](auto kernel) { launch_kernel(KC_PACK, kernel, dim3(blocks), dim3(kThreads), 0, s, a, table); };
+  auto launch = [&](auto kernel) { launch_kernel(KC_PACK, kernel, grid, dim3(kThreads), 0, s, a, table); };
   auto by_style = [&](auto k0, auto k1) { cfg->rope_style == 0 ? launch(k0) : launch(k1); };
   if (cfg->head_dim == 128)
     bits == 4 ? by_style(unpack_kernel<128, 4, 0>, unpack_kernel<128, 4, 1>) : by_style(unpack_kernel<128, 8, 0>, unpack_kernel<128, 8, 1>);
