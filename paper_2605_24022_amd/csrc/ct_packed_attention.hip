@@ -181,7 +181,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
   auto compute = [&](R& r, int blk) __attribute__((always_inline)) {
     // scores
     f32x4 s[2][NT];
-    const float k_scale[2] = {__uint_as_float((r.ks << 23) & 0x7f800000u), __uint_as_float((r.ks << 15) & 0x7f800000u)};
+    const float k_scale[2] = {scale_of(r.ks & 255u), scale_of(r.ks >> 8)};
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -286,10 +286,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
     // O^T += V^T P^T
     float v_scale[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t w = r.vs[i / 4];
-      v_scale[i] = __uint_as_float((i % 4 == 3 ? w >> 1 : w << (23 - 8 * (i % 4))) & 0x7f800000u);
-    }
+    for (int i = 0; i < 8; ++i) v_scale[i] = scale_of((r.vs[i / 4] >> (8 * (i % 4))) & 255u);
     static_for<MT / 2>([&](auto ec) __attribute__((always_inline)) {
       constexpr int E2 = decltype(ec)::value;
       uint32_t c[8];
@@ -469,11 +466,13 @@ struct PackedPlan {
 // cycles each; 0.36 with heads of 64) and the launch of the merge costs 3 us: sequences of up to 1024 rows stay
 // whole (one token, 32/8 heads of 128, 1, 4 and 16 sequences of 1024 rows: 7.4, 7.7 and 7.8 us whole, 7.7, 8.7 and
 // 10.8 in parts; 8/2 heads of 64 5.7 and 7.8; one of 2048 rows 11.3 and 8.1, 8.6 and 7.7).
-// Longer ones are divided until two workgroups stand on each compute unit, into parts of at least 128 rows.  Targets of
-// 256 / 512 / 768 / 1024 / 2048 workgroups, 4 bits: 64 sequences of 4096 rows - / 51 / 58 / 58 / 60 us (5.6 TB/s with
-// 512), 1 of 32768 14.1 / 15.3 / 15.9 / 17.5 / 20.1, 8 of up to 16384 with four tokens 32.3 / 30.3 / 32.7 / 34.9 / 35.4,
-// 2 of 131072 in 8 bits 97.5 / 96.5 / 99.6 / 99.0 / 104: three fit a compute unit, and beyond them a second round
-// starts that does not fill.
+// Longer ones are divided until a workgroup stands on each compute unit, into parts of at least 128 rows; where
+// parts would be longer than 4096 rows, until two do, because sequences of uneven length leave units idle for as long
+// as a part takes.  256 / 512 workgroups, 32/8 heads of 128, 4 bits, one token: one sequence of 8192 rows 10.2 / 10.5 us,
+// of 32768 13.8 / 15.2, of 65536 20.1 / 21.4; four of 8192 13.8 / 14.2, of 32768 30.9 / 31.9; but eight of 4096 to 16384
+// rows with four tokens 32.3 / 30.3, and two of 131072 in 8 bits 97.5 / 96.5.  768 and more are slower throughout (64
+// sequences of 4096 rows 51 us with 512, 58 with 768 and 1024): three workgroups fit a unit, and beyond them a second
+// round starts that does not fill.
 PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, int64_t max_len) {
   PackedPlan p;
   const int64_t n_cols = n_new * (cfg->n_q_heads / cfg->n_kv_heads);
@@ -481,9 +480,14 @@ PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, in
   p.col_blocks = (int)((n_cols + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
   const int64_t blocks = (max_len + kPackRows - 1) / kPackRows + 1;   // a sequence may start inside a block
   const int64_t groups = n_seq * cfg->n_kv_heads * p.col_blocks;
-  int64_t parts = blocks * p.col_tiles <= 33 ? 1 : (2 * kNumCUs + groups - 1) / groups;
-  int64_t per = (blocks + parts - 1) / parts;
+  auto blocks_per = [&](int64_t workgroups) {
+    const int64_t parts = (workgroups + groups - 1) / groups;
+    return (blocks + parts - 1) / parts;
+  };
+  int64_t per = blocks_per(kNumCUs);
+  if (per > 128) per = blocks_per(2 * kNumCUs);
   if (per < 4) per = 4;
+  if (blocks * p.col_tiles <= 33) per = blocks;
   p.part_blocks = (int)per;
   p.n_parts = (int)((blocks + per - 1) / per);
   p.o_bytes = (size_t)(n_seq * cfg->n_kv_heads * p.n_parts) * n_cols * cfg->head_dim * sizeof(float);
