@@ -1,7 +1,8 @@
 // Packed K/V cache: rows written in 4 or 8 bits (ct_pack_kv) and read back into layer buffers with the keys rotated to
 // their new positions (ct_unpack_kv; Eq. 8 in delta form, as for chunks cached in bf16).
 //
-// Both move every byte once.  A token of 8 heads of 128 is 4096 bytes in bf16 (K and V) and 1088 in 4 bits, 2112 in 8.
+// Bound: memory.  Both move every byte once: a token of 8 heads of 128 is 4096 bytes in bf16 (K and V) and 1088 in 4
+// bits, 2112 in 8.  32768 tokens to 4 bits and back: 59 us for 340 MB, 5.7 TB/s.
 #include "ct_packed.h"
 #include "ct_rotate.h"
 
@@ -24,8 +25,8 @@ struct PackArgs {
 };
 
 // A workgroup takes 32 tokens of one head (those of one block of the cache, where the rows are a run), so that every
-// line of the cache is written by one workgroup in whole: lines that several dies write in parts cost most of the
-// time.  A thread takes 8 elements at a time; threads lie along the row for K and along the tokens for V, which is the
+// line of codes is written by one workgroup in whole (a thread per 8 elements in the order of the rows, whose lines several
+// dies write in parts: 32768 tokens and back 80 us instead of 71).  A thread takes 8 elements at a time; threads lie along the row for K and along the tokens for V, which is the
 // order of their codes; the threads that share a scale are 1, 2 and 3 (K) or 8, 16 and 24 (V) apart.
 template <int D, int BITS>
 __global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
@@ -153,10 +154,10 @@ struct Packed8 {
 // A workgroup takes a tile of tokens (32, or 64 with heads of 64) and two heads.  K: a thread owns 8 rotation pairs of one
 // token, its sines and cosines serve both heads.  V: a thread takes 8 elements, threads along the tokens, the order of
 // the codes; both write whole lines.  One, two, four or eight heads per workgroup: 8192 tokens in 4 bits 9.5 / 8.0 / 8.2 /
-// 10.3 us, 31901 in 8 bits 37 / 33.9 / 36.2 / 37.1.
-// The stores do not stay in the caches: 8.0 against 9.7 us and 33.9 against 42.1 (5.0 TB/s), and what follows in a partial
-// prefill takes as long as the call wins or loses by it (unpack, projection, scatter and attention of 15 % of 31901 rows
-// 1281 us with either, of 5 % 500 against 497; of 8192 186.6 against 186.0).
+// 10.3 us (36 MB), 31901 in 8 bits 37 / 31.5 / 36 / 37 (169 MB, 5.4 TB/s; a large copy moves 5.1).
+// The stores do not stay in the caches: 8.0 against 9.7 us, and 33.9 against 42.1 when that was measured; what follows in
+// a partial prefill takes about as much longer as the call gains (unpack, projection, scatter and attention of 15 % of
+// 31901 rows 1281 us with either, of 5 % 500 against 497; of 15 % of 8192 186.6 against 186.0).
 constexpr int kUnpackHeads = 2;
 template <int D, int BITS, int STYLE>
 __global__ __launch_bounds__(kThreads) void unpack_kernel(UnpackArgs a, RopeTable table) {
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(UnpackArgs a, RopeTabl
     t_v[i] = t0 + i * STEP + tid / (8 * PIECES) * 8 + tid % 8;
     row_v[i] = row_of(t_v[i]);
   }
-  const int d_a = piece_a<D, STYLE>(jg), d_b = piece_b<D, STYLE>(jg), d_v = tid / 8 % PIECES * 8;
+  const int d_a = piece_a<D>(jg), d_b = piece_b<D>(jg), d_v = tid / 8 % PIECES * 8;
   // both heads are on their way while the angles are worked out
   struct Head {
     Packed8<D, BITS> ka, kb, v[2];
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(UnpackArgs a, RopeTabl
   if (turns && row_k >= 0) {
     const int32_t delta = a.new_pos[t_k] - (a.old_pos != nullptr ? a.old_pos[t_k] : 0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sincos_turns(delta, table.turns[jg * 8 + i], cs[i], sn[i]);
+    for (int i = 0; i < 8; ++i) sincos_turns(delta, table.turns[pair_of<D, STYLE>(jg, i)], cs[i], sn[i]);
   }
   auto finish = [&](const Head& x, int head) __attribute__((always_inline)) {
 #pragma unroll

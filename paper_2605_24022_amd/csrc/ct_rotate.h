@@ -6,11 +6,18 @@
 
 namespace ct {
 
-// Element offsets, inside a head row, of the two 16-byte pieces of the thread that owns pairs 8 jg .. 8 jg + 7.
+// A thread jg of the D / 16 of a head row owns the 16-byte pieces at elements 8 jg and D / 2 + 8 jg, neighbours next to
+// each other in both rotation styles, so that a store fills whole lines (with STYLE 1 pieces of one thread side by
+// side, streaming stores took up to 1.7 times as long).  Its pairs: STYLE 0 the elements (i, i + D / 2) of both pieces;
+// STYLE 1 four pairs (2 j, 2 j + 1) in each.  pair_of: the rotation pair, and so the frequency, of its pair i.
+template <int D>
+__device__ __forceinline__ int piece_a(int jg) { return jg * 8; }
+template <int D>
+__device__ __forceinline__ int piece_b(int jg) { return jg * 8 + D / 2; }
 template <int D, int STYLE>
-__device__ __forceinline__ int piece_a(int jg) { return STYLE == 0 ? jg * 8 : jg * 16; }
-template <int D, int STYLE>
-__device__ __forceinline__ int piece_b(int jg) { return STYLE == 0 ? jg * 8 + D / 2 : jg * 16 + 8; }
+__device__ __forceinline__ int pair_of(int jg, int i) {
+  return STYLE == 0 ? jg * 8 + i : jg * 4 + i % 4 + i / 4 * (D / 4);
+}
 
 __device__ __forceinline__ void widen8(u32x4 x, float (&f)[8]) {
 #pragma unroll
