@@ -340,15 +340,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
   const int64_t pair = (int64_t)b * a.Hkv + g;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
+    // (0 where no wave has a maximum: no key seen, and zeros for sums and weights, or scores that are all NaN, which stay
+    // NaN through a weight of zero)
     auto top_of = [&](int c) __attribute__((always_inline)) {
       float m = m_lds[0][c];
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) m = fmaxf(m, m_lds[w][c]);
-      return m;
+      return m == -INFINITY ? 0.f : m;
     };
     {
-      const float top = top_of(16 * n + l16);
-      const float f = m_run[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[n] - top);
+      const float f = __builtin_amdgcn_exp2f(m_run[n] - top_of(16 * n + l16));
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -368,15 +369,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
       for (int e = 0; e < PER / 4; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float m = m_lds[w][c];
-        total += m == -INFINITY ? 0.f : l_lds[w][c] * __builtin_amdgcn_exp2f(m - top);
+        total += l_lds[w][c] * __builtin_amdgcn_exp2f(m_lds[w][c] - top);
 #pragma unroll
         for (int e = 0; e < PER / 4; ++e) acc[e] += *reinterpret_cast<const f32x4*>(&o_lds[w][c_l][d0 + 4 * e]);
       }
       if (final) {
         const int t = col >> a.group_shift;
         const int64_t row = ((int64_t)b * a.n_new + t) * a.Hq + g * G + (col & (G - 1));
-        const float inv = top == -INFINITY ? 0.f : 1.0f / total;
+        const float inv = total == 0.f ? 0.f : 1.0f / total;
         uint32_t w[PER / 2];
 #pragma unroll
         for (int e = 0; e < PER / 2; ++e) w[e] = pack_bf16(acc[e / 2][e % 2 * 2] * inv, acc[e / 2][e % 2 * 2 + 1] * inv);
@@ -384,12 +384,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
         if constexpr (PER == 8) *reinterpret_cast<u32x4*>(op) = u32x4{w[0], w[1], w[2], w[3]};
         else *reinterpret_cast<u32x2*>(op) = u32x2{w[0], w[1]};
         if (a.lse != nullptr && d0 == 0)
-          a.lse[row] = top == -INFINITY ? -INFINITY : (top + __builtin_log2f(total)) * 0.69314718055994531f;
+          a.lse[row] = (top + __builtin_log2f(total)) * 0.69314718055994531f;      // (-inf where the sum is 0)
       } else {
         float* op = a.partial + ((pair * a.n_parts + part) * n_cols + col) * D + d0;
 #pragma unroll
         for (int e = 0; e < PER / 4; ++e) *reinterpret_cast<f32x4*>(op + 4 * e) = acc[e];
-        if (d0 == 0) reinterpret_cast<f32x2*>(a.partial_ml)[(pair * n_cols + col) * a.n_parts + part] = f32x2{top, total};
+        if (d0 == 0) reinterpret_cast<f32x2*>(a.partial_ml)[(pair * n_cols + col) * a.n_parts + part] = f32x2{total == 0.f ? -INFINITY : top, total};
       }
     }
     if (n + 1 < NT) __syncthreads();
@@ -423,10 +423,11 @@ __global__ __launch_bounds__(kMergeThreads) void packed_merge_kernel(PackedAttnA
   if ((tid & 63) == 0) red[tid >> 6] = top;
   __syncthreads();
   top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  if (top == -INFINITY) top = 0.f;                      // (as in the attention kernel)
   float total = 0.f;
   for (int i = tid; i < np; i += kMergeThreads) {
     const f32x2 x = ml[i];
-    const float w = x[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[0] - top);
+    const float w = __builtin_amdgcn_exp2f(x[0] - top);
     w_lds[i] = w;
     total += w * x[1];
   }
@@ -447,11 +448,11 @@ __global__ __launch_bounds__(kMergeThreads) void packed_merge_kernel(PackedAttnA
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < SLOTS; ++i) sum += *reinterpret_cast<const f32x4*>(&o_lds[i][tid * 4]);
-  const float inv = top == -INFINITY ? 0.f : 1.0f / total;
+  const float inv = total == 0.f ? 0.f : 1.0f / total;
   *reinterpret_cast<u32x2*>(a.out + row * D + tid * 4) =
       u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
   if (a.lse != nullptr && tid == 0)
-    a.lse[row] = top == -INFINITY ? -INFINITY : (top + __builtin_log2f(total)) * 0.69314718055994531f;
+    a.lse[row] = (top + __builtin_log2f(total)) * 0.69314718055994531f;
 }
 
 struct PackedPlan {

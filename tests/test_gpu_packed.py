@@ -324,6 +324,19 @@ def test_infinities_and_nan_reach_those_who_see_them(hq, hkv, d, bits, bad):
     _check_attention(hq, hkv, d, bits, 4, [301, 71, 50, 3], [16, 400, 600, 394], 704, edit=edit)
 
 
+@pytest.mark.parametrize("n_new,lens,nan_keys", [
+    (1, [1, 40], [0]),                                # nothing but a NaN
+    (1, [128, 40], list(range(32, 64))),              # all that one wave sees
+    (2, [2, 3], [1]),                                 # the earlier token sees none of it
+    (1, [6000, 40], list(range(2048, 4096))),         # all that one part of the key range holds
+    (1, [6000, 40], list(range(6000)))])
+def test_keys_that_are_all_nan(n_new, lens, nan_keys):
+    """Scores that are all NaN leave no maximum behind: output and log-sum-exp are NaN all the same."""
+    def edit(k, v):
+        k[5 + np.array(nan_keys)] = 0x7fc0
+    _check_attention(8, 2, 64, 4, n_new, lens, [5, 6050], 6112, edit=edit)
+
+
 def test_without_lse():
     _check_attention(8, 2, 64, 4, 1, [3000, 20], [0, 3000], 3040, with_lse=False)
 
