@@ -18,6 +18,9 @@ constexpr int kNumXCDs = 8;     // accelerator dies; consecutive workgroup ids o
 // the round).
 constexpr int kCUsHeldPerStreamInBlock = 4;
 
+// A launch holds fewer than 2^32 threads: workgroups of 256 that one may have.
+constexpr int64_t kMaxWorkgroups = 0xffffffffll / 256;
+
 // ---- kernel classes for the opt-in event profiling ------------------------------------
 enum KernelClass { KC_QKV = 0, KC_REROPE = 1, KC_SCATTER = 2, KC_ATTN = 3, KC_MERGE = 4, KC_LINEAR = 5, KC_NORM = 6, KC_FREQ = 7, KC_TOPK = 8, KC_PACK = 9, KC_PACKED_ATTN = 10, KC_COUNT = 11 };
 

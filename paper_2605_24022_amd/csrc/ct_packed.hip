@@ -279,7 +279,7 @@ ct_status ct_pack_kv(const ct_layer_cfg* cfg, const void* k, int64_t k_stride, c
   PackArgs a = {static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), k_stride, v_stride, rows, first_row, n_tokens,
                 static_cast<unsigned char*>(cache), n_rows, cfg->n_kv_heads};
   const int64_t tiles = ((rows != nullptr ? 0 : first_row % kPackRows) + (int64_t)n_tokens + kPackRows - 1) / kPackRows;
-  if (tiles * cfg->n_kv_heads > 0x7fffffff)
+  if (tiles * cfg->n_kv_heads > kMaxWorkgroups)
     return fail(CT_ERR_UNSUPPORTED, "n_tokens %d x %d heads are too many for one launch", n_tokens, cfg->n_kv_heads);
   const dim3 grid((unsigned)(tiles * cfg->n_kv_heads));
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -306,8 +306,10 @@ ct_status ct_unpack_kv(const ct_layer_cfg* cfg, const void* cache, int32_t n_row
   UnpackArgs a = {static_cast<const unsigned char*>(cache), n_rows, cfg->n_kv_heads, rows, first_row, old_pos, new_pos, n_tokens,
                   static_cast<uint16_t*>(k_dst), static_cast<uint16_t*>(v_dst)};
   const int tile = kThreads / (cfg->head_dim / 16);
-  const unsigned tiles = (unsigned)(((int64_t)n_tokens + tile - 1) / tile);
-  const dim3 grid(tiles, (unsigned)((cfg->n_kv_heads + kUnpackHeads - 1) / kUnpackHeads));
+  const int64_t tiles = ((int64_t)n_tokens + tile - 1) / tile, head_tiles = (cfg->n_kv_heads + kUnpackHeads - 1) / kUnpackHeads;
+  if (tiles > kMaxWorkgroups || head_tiles > 0xffff)
+    return fail(CT_ERR_UNSUPPORTED, "n_tokens %d x %d heads are too many for one launch", n_tokens, cfg->n_kv_heads);
+  const dim3 grid((unsigned)tiles, (unsigned)head_tiles);
   RopeTable table;
   fill_rope_table(cfg, &table);
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -500,7 +500,7 @@ ct_status check_attn_sizes(const ct_layer_cfg* cfg, int32_t n_seq, int32_t n_new
   if (n_seq < 0 || max_len < 0) return fail(CT_ERR_SHAPE, "negative size (n_seq %d, max_len %d)", n_seq, max_len);
   if (n_new < 1) return fail(CT_ERR_SHAPE, "n_new %d must be at least 1", n_new);
   if (n_new > 64) return fail(CT_ERR_UNSUPPORTED, "n_new %d: at most 64 new tokens per sequence", n_new);
-  if ((int64_t)n_seq * n_new * cfg->n_q_heads > 0x7fffffff)
+  if ((int64_t)n_seq * n_new * cfg->n_q_heads > kMaxWorkgroups)      // (of the merge, one per row)
     return fail(CT_ERR_UNSUPPORTED, "n_seq %d x n_new %d x %d heads are too many rows for one launch", n_seq, n_new, cfg->n_q_heads);
   return CT_OK;
 }
@@ -532,7 +532,7 @@ ct_status ct_packed_attention(const ct_layer_cfg* cfg, const void* q, int32_t n_
     return fail(CT_ERR_UNSUPPORTED, "q, cache and out must be 16-byte aligned");
   const PackedPlan p = plan_packed(cfg, n_seq, n_new, max_len);
   const int64_t groups = (int64_t)n_seq * cfg->n_kv_heads * p.col_blocks * p.n_parts;
-  if (groups > 0x7fffffff) return fail(CT_ERR_UNSUPPORTED, "n_seq %d with max_len %d: too many workgroups", n_seq, max_len);
+  if (groups > kMaxWorkgroups) return fail(CT_ERR_UNSUPPORTED, "n_seq %d with max_len %d: too many workgroups", n_seq, max_len);
   if (p.ws_bytes > 0) {
     if (workspace == nullptr) return fail(CT_ERR_WORKSPACE, "workspace is NULL but %zu bytes are needed", p.ws_bytes);
     if (workspace_bytes < p.ws_bytes)

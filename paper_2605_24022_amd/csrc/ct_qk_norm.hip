@@ -103,7 +103,7 @@ ct_status ct_qk_norm_rope(const ct_layer_cfg* cfg, const void* qkv, const int32_
                   static_cast<uint16_t*>(v_out), n_tokens, cfg->n_q_heads, cfg->n_kv_heads,
                   cfg->n_q_heads + (v_out != nullptr ? 2 : 1) * cfg->n_kv_heads, eps};
   const int64_t blocks = ((int64_t)n_tokens * a.heads * (cfg->head_dim / 16) + kThreads - 1) / kThreads;
-  if (blocks > 0x7fffffff) return fail(CT_ERR_UNSUPPORTED, "n_tokens %d x %d heads are too many for one launch", n_tokens, a.heads);
+  if (blocks > kMaxWorkgroups) return fail(CT_ERR_UNSUPPORTED, "n_tokens %d x %d heads are too many for one launch", n_tokens, a.heads);
   RopeTable table;
   fill_rope_table(cfg, &table);
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -166,6 +166,17 @@ def test_attention_refusals():
     B.ct_packed_attention(c, None, 0, 1, None, 64, 4, None, None, 64, None, None, None, 0)
 
 
+def test_launches_beyond_what_a_grid_holds_are_refused():
+    """A launch has fewer than 2^32 threads."""
+    c, most = _cfg(), 2 ** 31 - 1
+    assert _status(B.ct_pack_kv, c, FAKE, 1024, FAKE, 1024, most, FAKE, 0, FAKE, 64, 4) == B.CT_ERR_UNSUPPORTED
+    assert _status(B.ct_unpack_kv, c, FAKE, 64, 4, FAKE, 0, None, None, most, FAKE, FAKE) == B.CT_ERR_UNSUPPORTED
+    assert _status(B.ct_qk_norm_rope, c, FAKE, FAKE, most, FAKE, FAKE, 0.0, FAKE, FAKE, FAKE) == B.CT_ERR_UNSUPPORTED
+    rows = 2 ** 32 // 256 // 32                                                 # sequences whose rows just do not fit
+    assert _status(B.ct_packed_attention, c, FAKE, rows, 1, FAKE, 64, 4, FAKE, FAKE, 64, FAKE, None, None, 0) == B.CT_ERR_UNSUPPORTED
+    assert _status(B.ct_packed_attention, c, FAKE, rows - 1, 1, FAKE, 64, 4, FAKE, FAKE, 64, None, None, None, 0) == B.CT_ERR_NULL
+
+
 def test_qk_norm_refusals():
     c = _cfg()
 
