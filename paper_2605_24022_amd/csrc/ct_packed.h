@@ -14,6 +14,8 @@
 //   V codes   [4 key groups][16 lanes][8 rows][D / 16]: the A operand of O^T += V^T P^T wants 8 keys of one
 //             dimension in a lane; a lane that holds 8 keys x D / 16 dimensions gets there with one v_perm per
 //             pair of elements, and nothing goes through LDS
+// Lanes load 16 bytes at a time; where a lane's share is longer, the first 16 bytes of all lanes lie together, then the
+// second (so that streaming loads, which do not find the rest of a line in a cache, use it whole).
 //   K scales  [D / 32][32], rows in the order in which a lane of the two 16-key MFMA tiles needs them
 //   V scales  [D / 32][32 rows]
 #pragma once
@@ -38,9 +40,16 @@ struct PackLayout {
   static constexpr int kLaneDims = D / 16;                     // V dimensions per lane
   static constexpr int kLaneBytes = kLaneDims * BITS / 8;      // of one key
 
-  static __device__ __forceinline__ int k_code(int row, int dim) { return row * kRowBytes + dim * BITS / 8; }
+  // A lane's share of a K row or of V (16, 32 or 64 bytes, or 8) lies in quads of 16 bytes, the same quad of neighbouring
+  // lanes side by side.
+  static constexpr int kShareK = kRowBytes / 4, kShareV = 8 * kLaneBytes;
+  static __device__ __forceinline__ int k_code(int row, int dim) {
+    const int byte = dim * BITS / 8, in = byte % kShareK;
+    return row * kRowBytes + (kShareK <= 16 ? byte : in / 16 * 64 + byte / kShareK * 16 + in % 16);
+  }
   static __device__ __forceinline__ int v_code(int row, int dim) {
-    return kVCodes + (((row >> 3) * 16 + dim / kLaneDims) * 8 + (row & 7)) * kLaneBytes + dim % kLaneDims * BITS / 8;
+    const int lane = (row >> 3) * 16 + dim / kLaneDims, in = (row & 7) * kLaneBytes + dim % kLaneDims * BITS / 8;
+    return kVCodes + in / 16 * 1024 + lane * 16 + in % 16;
   }
   static __device__ __forceinline__ int k_scale(int row, int group) {
     return kKScales + group * kPackRows + (row & 24) + (row & 3) * 2 + ((row >> 2) & 1);

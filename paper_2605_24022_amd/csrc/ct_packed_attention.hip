@@ -33,7 +33,7 @@ struct PackedAttnArgs {
   float* partial_ml;              // and its (m, l): [sequence, KV head][column][part]
   int32_t n_seq, n_new, n_rows, max_len;
   int32_t Hq, Hkv, group_shift;   // query heads per KV head: 1 << group_shift
-  int32_t n_parts, part_blocks;   // parts of the key range, and blocks of 32 rows in each
+  int32_t n_parts, part_blocks;   // most parts of a key range, and the blocks of 32 rows in each, about
   int32_t col_blocks;
   float scale_log2;               // softmax scale * log2(e)
 };
@@ -87,12 +87,14 @@ struct Raw {
   uint32_t vs[2];   // eight
 };
 
-template <int W>
+// (STRIDE: bytes between the 16-byte quads of a lane)
+template <int STRIDE, bool STREAM, int W>
 __device__ __forceinline__ void load_words(uint32_t (&dst)[W], const unsigned char* p) {
   if constexpr (W % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < W; i += 4) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(p + 4 * i);
+      const u32x4* q = reinterpret_cast<const u32x4*>(p + i / 4 * STRIDE);
+      const u32x4 x = STREAM ? __builtin_nontemporal_load(q) : *q;
       dst[i] = x[0]; dst[i + 1] = x[1]; dst[i + 2] = x[2]; dst[i + 3] = x[3];
     }
   } else {
@@ -109,9 +111,10 @@ __device__ __forceinline__ uint32_t v_pair(const uint32_t* v, float scale) {
   return unpack_pair<BITS, BITS == 4 ? byte % 4 : byte % 4 / 2>(v[byte / 4], scale);
 }
 
-template <int D, int BITS, int NT>
+// STREAM: loads of codes that do not stay in the caches (see stream_loads).
 // Registers for three waves per SIMD (16 columns) or two (32): left alone the compiler keeps the accumulators in
 // registers of their own and two waves, or one, remain.
+template <int D, int BITS, int NT, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT == 1 ? 3 : 2))) void packed_attn_kernel(PackedAttnArgs a) {
   using L = PackLayout<D, BITS>;
   using R = Raw<D, BITS>;
@@ -128,7 +131,6 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
   const int b = rest / a.n_parts;
   const Sequence seq = sequence_of(a, b);
   if (part >= max(seq.n_parts, 1)) return;            // (an empty sequence still gets its zeros, from part 0)
-  const int blk0 = seq.b0 + part * a.part_blocks, blk1 = min(blk0 + a.part_blocks, seq.b1);
 
   // ---- this lane's columns: column c is head c mod G of new token c / G --------------------------------
   const int G = 1 << a.group_shift;
@@ -149,21 +151,21 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
 
   // ---- where a lane finds its share of a block -------------------------------------------------------
   const int k_row = 8 * (l16 >> 2) + (l16 & 3);       // row of 16-key tile 0; tile 1: 4 rows further on
-  const int k_off = k_row * L::kRowBytes + h * (L::kRowBytes / 4);
+  const int k_off = k_row * L::kRowBytes + h * (L::kShareK < 16 ? L::kShareK : 16);
   const int out_group = h * (D / 4) / kPackGroup;     // scale group of the K dimensions, and of the output dimensions
   const int ks_off = L::kKScales + out_group * kPackRows + 2 * l16;
-  const int v_off = L::kVCodes + (h * 16 + l16) * 8 * L::kLaneBytes;
+  const int v_off = L::kVCodes + lane * 16;
   const int vs_off = L::kVScales + l16 * MT / kPackGroup * kPackRows + 8 * h;
   auto block_ptr = [&](int blk) __attribute__((always_inline)) {
     return a.cache + ((int64_t)blk * a.Hkv + g) * L::kBytes;
   };
   auto load = [&](R& r, int blk) __attribute__((always_inline)) {
     const unsigned char* p = block_ptr(blk);
-    load_words(r.k[0], p + k_off);
-    load_words(r.k[1], p + k_off + 4 * L::kRowBytes);
+    load_words<64, STREAM>(r.k[0], p + k_off);
+    load_words<64, STREAM>(r.k[1], p + k_off + 4 * L::kRowBytes);
     r.ks = *reinterpret_cast<const uint16_t*>(p + ks_off);
-    load_words(r.v, p + v_off);
-    load_words(r.vs, p + vs_off);
+    load_words<1024, STREAM>(r.v, p + v_off);
+    load_words<0, false>(r.vs, p + vs_off);
   };
 
   // ---- state -----------------------------------------------------------------------------------------
@@ -309,16 +311,20 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
   };
 
   // ---- the blocks of this wave, the next one on its way while one is worked on ---------------------------------
+  // The parts of a sequence take four blocks in turn and so walk through the same stretch of memory together (each a
+  // range of its own: 2 sequences of 131072 rows in 8 bits 87.5 us instead of 85.4, one of 32768 13.6 instead of 13.3).
+  const int step = kWaves * max(seq.n_parts, 1), blk1 = seq.b1;
   // (Two or three blocks ahead instead of one: within 3 % of this with 4-bit codes, registers spill with 8-bit ones.)
-  if (blk0 + wave < blk1) {
+  const int blk0 = seq.b0 + part * kWaves + wave;
+  if (blk0 < blk1) {
     R r[2];
-    load(r[0], blk0 + wave);
-    for (int blk = blk0 + wave; blk < blk1;) {
+    load(r[0], blk0);
+    for (int blk = blk0; blk < blk1;) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        load(r[1 - i], min(blk + kWaves, blk1 - 1));
+        load(r[1 - i], min(blk + step, blk1 - 1));
         compute(r[i], blk);
-        blk += kWaves;
+        blk += step;
         if (blk >= blk1) break;
       }
     }
@@ -455,6 +461,15 @@ __global__ __launch_bounds__(kMergeThreads) void packed_merge_kernel(PackedAttnA
     a.lse[row] = (top + __builtin_log2f(total)) * 0.69314718055994531f;
 }
 
+// Codes that are read once stream past the caches: 64 sequences of 4096 rows 50.8 -> 46.1 us in 4 bits (6.2 TB/s), of 2048
+// rows 48.4 -> 44.0 in 8, 2 of 131072 in 8 94.5 -> 85.4.  What several workgroups read suffers in 8 bits, not in 4: 16
+// sequences of 8192 rows with 64 columns in two workgroups 76.6 -> 92.1 (60.7 -> 59.1), 64 sequences that are the same
+// 32768 rows 304 -> 419 (215 -> 217).  So 8-bit codes stream where one workgroup holds all columns and the cache has
+// rows enough for no two sequences to share any.
+bool stream_loads(int bits, int col_blocks, int64_t n_seq, int64_t max_len, int64_t n_rows) {
+  return bits == 4 || (col_blocks == 1 && n_seq * max_len <= n_rows);
+}
+
 struct PackedPlan {
   int col_tiles;      // 16-column tiles per workgroup
   int col_blocks;
@@ -566,12 +581,16 @@ ct_status ct_packed_attention(const ct_layer_cfg* cfg, const void* q, int32_t n_
     launch_kernel(KC_PACKED_ATTN, kernel, dim3((unsigned)groups), dim3(64 * kWaves), 0, s, a);
   };
   auto by_cols = [&](auto one, auto two) { p.col_tiles == 1 ? launch(one) : launch(two); };
-  if (cfg->head_dim == 128)
-    bits == 4 ? by_cols(packed_attn_kernel<128, 4, 1>, packed_attn_kernel<128, 4, 2>)
-              : by_cols(packed_attn_kernel<128, 8, 1>, packed_attn_kernel<128, 8, 2>);
-  else
-    bits == 4 ? by_cols(packed_attn_kernel<64, 4, 1>, packed_attn_kernel<64, 4, 2>)
-              : by_cols(packed_attn_kernel<64, 8, 1>, packed_attn_kernel<64, 8, 2>);
+  const bool stream_in = stream_loads(bits, p.col_blocks, n_seq, max_len, n_rows);
+  if (cfg->head_dim == 128) {
+    if (bits == 4) by_cols(packed_attn_kernel<128, 4, 1, true>, packed_attn_kernel<128, 4, 2, true>);
+    else if (stream_in) by_cols(packed_attn_kernel<128, 8, 1, true>, packed_attn_kernel<128, 8, 2, true>);
+    else by_cols(packed_attn_kernel<128, 8, 1, false>, packed_attn_kernel<128, 8, 2, false>);
+  } else {
+    if (bits == 4) by_cols(packed_attn_kernel<64, 4, 1, true>, packed_attn_kernel<64, 4, 2, true>);
+    else if (stream_in) by_cols(packed_attn_kernel<64, 8, 1, true>, packed_attn_kernel<64, 8, 2, true>);
+    else by_cols(packed_attn_kernel<64, 8, 1, false>, packed_attn_kernel<64, 8, 2, false>);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "packed attention kernel launch");
   if (p.n_parts > 1) {
