@@ -2,7 +2,9 @@
 // a partial prefill, one token (or a few drafted ones) per sequence at a time.
 //
 // Bound: the cache is read once and used for few queries, so memory decides as long as the conversion of the codes
-// keeps up: an element costs one conversion instruction per two, and V one v_perm per two besides.
+// keeps up: an element costs one conversion instruction per two, and V one v_perm per two besides.  64 sequences of
+// 4096 rows (32/8 heads of 128) 46 us in 4 bits, 6.2 TB/s; 2 of 131072 in 8 bits 85 us, 6.5 TB/s (a large copy moves
+// 5.1); short calls are a launch of 5 us, and a merge of 4 behind it where the key range is divided.
 //
 // Formulation, as in the selected-row attention: S^T = K Q^T and O^T += V^T P^T on 16 x 16 x 32 matrix instructions,
 // the columns being the G query heads of a KV head times the new tokens.  The cache's layout hands a lane its
@@ -480,15 +482,15 @@ struct PackedPlan {
 
 // How the key range is divided.  One wave takes about 0.5 us for a block of 32 rows (260 vector instructions at 4
 // cycles each; 0.36 with heads of 64) and the launch of the merge costs 3 us: sequences of up to 1024 rows stay
-// whole (one token, 32/8 heads of 128, 1, 4 and 16 sequences of 1024 rows: 7.4, 7.7 and 7.8 us whole, 7.7, 8.7 and
-// 10.8 in parts; 8/2 heads of 64 5.7 and 7.8; one of 2048 rows 11.3 and 8.1, 8.6 and 7.7).
+// whole (one token, 32/8 heads of 128, 1, 4 and 16 sequences of 1024 rows: 7.7, 8.3 and 8.5 us whole, 8.1, 8.7 and
+// 10.5 in parts; 8/2 heads of 64 5.7 and 7.7; one of 2048 rows 12.6 and 8.5, 8.5 and 7.6).
 // Longer ones are divided until a workgroup stands on each compute unit, into parts of at least 128 rows; where
 // parts would be longer than 4096 rows, until two do, because sequences of uneven length leave units idle for as long
-// as a part takes.  256 / 512 workgroups, 32/8 heads of 128, 4 bits, one token: one sequence of 8192 rows 10.2 / 10.5 us,
-// of 32768 13.8 / 15.2, of 65536 20.1 / 21.4; four of 8192 13.8 / 14.2, of 32768 30.9 / 31.9; but eight of 4096 to 16384
-// rows with four tokens 32.3 / 30.3, and two of 131072 in 8 bits 97.5 / 96.5.  768 and more are slower throughout (64
-// sequences of 4096 rows 51 us with 512, 58 with 768 and 1024): three workgroups fit a unit, and beyond them a second
-// round starts that does not fill.
+// as a part takes.  256 / 512 workgroups, 32/8 heads of 128, 4 bits, one token: one sequence of 8192 rows 10.4 / 10.5 us,
+// of 32768 13.0 / 14.6, of 65536 18.1 / 19.8; four of 8192 12.8 / 13.5, of 32768 28.3 / 29.0, two of 131072 in 8 bits
+// 83.6 / 85.3; but eight of 4096 to 16384 rows with four tokens 29.7 / 26.9.  768 are slower throughout (64 sequences of
+// 4096 rows 46 us with 512, 52 with 768): three workgroups fit a unit, and beyond them a second round starts that does
+// not fill.
 PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, int64_t max_len) {
   PackedPlan p;
   const int64_t n_cols = n_new * (cfg->n_q_heads / cfg->n_kv_heads);
