@@ -310,8 +310,8 @@ ct_status ct_unpack_kv(const ct_layer_cfg* cfg, const void* cache, int32_t n_row
   if (tiles > kMaxWorkgroups || head_tiles > 0xffff)
     return fail(CT_ERR_UNSUPPORTED, "n_tokens %d x %d heads are too many for one launch", n_tokens, cfg->n_kv_heads);
   const dim3 grid((unsigned)tiles, (unsigned)head_tiles);
-  RopeTable table;
-  fill_rope_table(cfg, &table);
+  RopeTable table = {};
+  if (new_pos != nullptr) fill_rope_products(cfg, &table);
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto launch = [&](auto kernel) { launch_kernel(KC_PACK, kernel, grid, dim3(kThreads), 0, s, a, table); };
   auto by_style = [&](auto k0, auto k1) { cfg->rope_style == 0 ? launch(k0) : launch(k1); };

@@ -105,7 +105,7 @@ ct_status ct_qk_norm_rope(const ct_layer_cfg* cfg, const void* qkv, const int32_
   const int64_t blocks = ((int64_t)n_tokens * a.heads * (cfg->head_dim / 16) + kThreads - 1) / kThreads;
   if (blocks > kMaxWorkgroups) return fail(CT_ERR_UNSUPPORTED, "n_tokens %d x %d heads are too many for one launch", n_tokens, a.heads);
   RopeTable table;
-  fill_rope_table(cfg, &table);
+  fill_rope_products(cfg, &table);
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto launch = [&](auto kernel) { launch_kernel(KC_NORM, kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, table); };
   if (cfg->head_dim == 128) cfg->rope_style == 0 ? launch(qk_norm_rope_kernel<128, 0>) : launch(qk_norm_rope_kernel<128, 1>);

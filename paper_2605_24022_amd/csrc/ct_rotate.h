@@ -2,9 +2,21 @@
 // queries and keys.
 #pragma once
 
+#include <math.h>
+
 #include "ct_internal.h"
 
 namespace ct {
+
+// The frequencies of fill_rope_table as products of theta^(-2 2^i / D): six powers instead of 64, because calls with few
+// rows last as long as the host takes to launch them (0.45 us of 5).  Six roundings in fp64 at most: 1e-9 rad at position
+// 2^20.
+inline void fill_rope_products(const ct_layer_cfg* cfg, RopeTable* t) {
+  double step[6];
+  for (int i = 0; i < 6; ++i) step[i] = pow(cfg->rope_theta, -2.0 * (double)(1 << i) / (double)cfg->head_dim);
+  t->turns[0] = 1.0 / 6.283185307179586476925286766559;
+  for (int j = 1; j < 64; ++j) t->turns[j] = t->turns[j & (j - 1)] * step[__builtin_ctz(j)];
+}
 
 // A thread jg of the D / 16 of a head row owns the 16-byte pieces at elements 8 jg and D / 2 + 8 jg, neighbours next to
 // each other in both rotation styles, so that a store fills whole lines (with STYLE 1 pieces of one thread side by
