@@ -63,6 +63,12 @@ inline size_t pack_block_bytes(const ct_layer_cfg* cfg, int bits) {
 
 #if defined(__HIPCC__)
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// Scale byte I of a word.  The conversions look at the exponent of their scale alone (checked: all 256 bytes with 64
+// patterns in sign and mantissa), so the other bytes may stay.
+template <int I>
+__device__ __forceinline__ float scale_in(uint32_t w) {
+  return __uint_as_float(I == 3 ? w >> 1 : w << (23 - 8 * I));
+}
 
 // Byte (two elements, 4 bits each) or halfword (8 bits each) PART of a word of codes, scaled, as a pair of bf16.
 template <int BITS, int PART>

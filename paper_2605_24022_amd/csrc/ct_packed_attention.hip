@@ -153,11 +153,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
 
   // ---- where a lane finds its share of a block -------------------------------------------------------
   const int k_row = 8 * (l16 >> 2) + (l16 & 3);       // row of 16-key tile 0; tile 1: 4 rows further on
-  const int k_off = k_row * L::kRowBytes + h * (L::kShareK < 16 ? L::kShareK : 16);
+  const uint32_t k_off = k_row * L::kRowBytes + h * (L::kShareK < 16 ? L::kShareK : 16);
   const int out_group = h * (D / 4) / kPackGroup;     // scale group of the K dimensions, and of the output dimensions
-  const int ks_off = L::kKScales + out_group * kPackRows + 2 * l16;
-  const int v_off = L::kVCodes + lane * 16;
-  const int vs_off = L::kVScales + l16 * MT / kPackGroup * kPackRows + 8 * h;
+  const uint32_t ks_off = L::kKScales + out_group * kPackRows + 2 * l16;
+  const uint32_t v_off = L::kVCodes + lane * 16;
+  const uint32_t vs_off = L::kVScales + l16 * MT / kPackGroup * kPackRows + 8 * h;
   auto block_ptr = [&](int blk) __attribute__((always_inline)) {
     return a.cache + ((int64_t)blk * a.Hkv + g) * L::kBytes;
   };
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
   auto compute = [&](R& r, int blk) __attribute__((always_inline)) {
     // scores
     f32x4 s[2][NT];
-    const float k_scale[2] = {scale_of(r.ks & 255u), scale_of(r.ks >> 8)};
+    const float k_scale[2] = {scale_in<0>(r.ks), scale_in<1>(r.ks)};
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -202,35 +202,41 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
     // sequence may hold anything, rows that only some columns see may hold NaN.
     const int32_t row0 = blk * kPackRows;
     if (row0 < seq.first || row0 + kPackRows - 1 > first_last) {
-      const int lo = seq.first - row0 - 8 * h, hi = seq.end - row0 - 8 * h;   // keys [lo, hi) of the lane's eight are the sequence's
+      // Bit i of a mask stands for key 8h + i.  (Masks of bits in vector registers: comparisons key by key need more
+      // scalar registers for their results than there are.)
+      auto bits_below = [](int n) __attribute__((always_inline)) { return (1u << min(max(n, 0), 8)) - 1u; };
+      auto spread = [](uint32_t bits, int i) __attribute__((always_inline)) { return (uint32_t)((int32_t)(bits << (31 - i)) >> 31); };
+      const int base = row0 + 8 * h;
+      const uint32_t from_first = ~bits_below(seq.first - base), in = from_first & bits_below(seq.end - base);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const int rel = last[n] - row0 - 8 * h;
+        const uint32_t seen = from_first & bits_below(last[n] + 1 - base);
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            s[u][n][i] = 4 * u + i < lo || 4 * u + i > rel ? -INFINITY : s[u][n][i];
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t m = spread(seen, i);
+          s[i / 4][n][i % 4] = __uint_as_float((__float_as_uint(s[i / 4][n][i % 4]) & m) | (0xff800000u & ~m));
+        }
       }
       // A probability of zero does not silence a NaN: such elements of V become zeros here, and NaN goes to the
       // columns that do see one.
-      bool nan = false;
-      static_for<8>([&](auto sc) __attribute__((always_inline)) {
-        constexpr int S = decltype(sc)::value, SH = 8 * (S % 4);
-        const bool in = S >= lo && S < hi, is_nan = ((r.vs[S / 4] >> SH) & 255u) == kScaleNaN;
-        nan |= in && is_nan;
-        if (!in || is_nan) {
-          r.vs[S / 4] = (r.vs[S / 4] & ~(255u << SH)) | 127u << SH;
-          constexpr int B0 = S * L::kLaneBytes;
-          if constexpr (L::kLaneBytes == 2) {
-            r.v[B0 / 4] &= B0 % 4 == 0 ? 0xffff0000u : 0x0000ffffu;
-          } else {
+      uint32_t nan = 0;      // scale bytes of 255
 #pragma unroll
-            for (int w = 0; w < L::kLaneBytes / 4; ++w) r.v[B0 / 4 + w] = 0u;
-          }
-        }
-      });
-      if (__any(nan)) {
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t top = ((r.vs[w] & 0x7f7f7f7fu) + 0x01010101u) & r.vs[w] & 0x80808080u;
+        nan |= ((top >> 7) * 0x10204080u >> 28) << (4 * w);      // bits 0, 8, 16, 24 next to one another
+      }
+      const uint32_t keep = in & ~nan;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t bytes = ((keep >> (4 * w) & 15u) * 0x00204081u & 0x01010101u) * 255u;
+        r.vs[w] = (r.vs[w] & bytes) | (0x7f7f7f7fu & ~bytes);
+      }
+#pragma unroll
+      for (int w = 0; w < R::VW; ++w) {
+        if constexpr (L::kLaneBytes == 2) r.v[w] &= (spread(keep, 2 * w) & 0xffffu) | spread(keep, 2 * w + 1) << 16;
+        else r.v[w] &= spread(keep, 4 * w / L::kLaneBytes);
+      }
+      if (__any((in & nan) != 0)) {
         const unsigned char* vs = block_ptr(blk) + L::kVScales + out_group * kPackRows;
         bool sees[NT] = {};
 #pragma unroll 1
@@ -283,14 +289,17 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][n][i % 4], a.scale_log2, -m_use));
       l_run[n] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-      // bf16 operands: half a step is 2^-9 of a probability, independent from key to key; the sum above is unrounded
+      // bf16 operands: off by up to half a step, 2^-8 of a probability, independently from key to key; the sum above is
+      // unrounded.  (A second product for what the rounding leaves: 3 to 6 % slower, 10 % with 8-bit codes.)
       const u32x4 w = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
       pf[n] = __builtin_bit_cast(bf16x8, w);
     }
     // O^T += V^T P^T
     float v_scale[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v_scale[i] = scale_of((r.vs[i / 4] >> (8 * (i % 4))) & 255u);
+    static_for<8>([&](auto sc) __attribute__((always_inline)) {
+      constexpr int S = decltype(sc)::value;
+      v_scale[S] = scale_in<S % 4>(r.vs[S / 4]);
+    });
     static_for<MT / 2>([&](auto ec) __attribute__((always_inline)) {
       constexpr int E2 = decltype(ec)::value;
       uint32_t c[8];
