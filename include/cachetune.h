@@ -401,10 +401,11 @@ ct_status ct_select_frequency(const void* k, const void* v, int32_t n_batch, int
  *   bits 4   to one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign (e2m1; emax 2)
  *   bits 8   to three mantissa bits, at most 448, steps of 2^-9 at least, and a sign (e4m3; emax 8)
  * (magnitudes above 1.75 * 2^127 count as that, so that finite elements come back finite).  4.25 and 8.25 bits per
- * element with the scales.  32 elements that hold an infinity or a NaN read back as NaN, all
- * of them.  The bytes of 32 consecutive rows from a multiple of 32 on are contiguous, so such runs may be moved by plain
- * copies of n / n_rows of the cache's bytes, between devices and host pools too; the layout inside is the
- * library's own.  A cache's bytes are undefined until rows are written; only rows that were written may be read. */
+ * element with the scales.  32 elements that hold an infinity or a NaN read back as NaN, all of them.
+ * Rows lie in blocks of 32: n rows (a multiple of 32) from a multiple of 32 on are one piece of
+ * ct_packed_kv_bytes(cfg, n, bits) bytes, which may be copied to a multiple of 32 of another cache, through host pools
+ * too; the layout inside is the library's own.  A cache's bytes are undefined until rows are written; only rows that
+ * were written may be read. */
 
 /* Bytes of a packed cache; 0 for invalid arguments.  Host function. */
 size_t ct_packed_kv_bytes(const ct_layer_cfg* cfg, int32_t n_rows, int32_t bits);

@@ -143,6 +143,25 @@ def test_rows_inside_projected_rows(d, bits):
     assert np.isnan(gk[:3]).all() and np.isnan(gv[3 + n:]).all()               # not written
 
 
+@pytest.mark.parametrize("hkv,d,bits", [(2, 64, 4), (8, 128, 8)])
+def test_blocks_of_rows_are_copied_as_bytes(hkv, d, bits):
+    """Rows 64 to 127 of one cache become rows 32 to 95 of another, by way of pinned host memory."""
+    say(f"packed blocks copied hkv={hkv} d={d} bits={bits}")
+    rng = np.random.default_rng([hkv, d, bits])
+    cfg, per = _cfg(hkv, hkv, d), B.ct_packed_kv_bytes(_cfg(hkv, hkv, d), 32, bits)
+    one, other = _cache(cfg, 160, bits), _cache(cfg, 128, bits)
+    k, v = _bits(rng, 160, hkv, d), _bits(rng, 160, hkv, d)
+    _pack(cfg, k, v, one, 160, bits)
+    assert B.ct_packed_kv_bytes(cfg, 64, bits) == 2 * per
+    host = torch.empty(2 * per, dtype=torch.uint8, pin_memory=True)
+    host.copy_(one[2 * per:4 * per])
+    other[per:3 * per].copy_(host)
+    gk, gv = _read(cfg, other, 128, bits, hkv, d)
+    for got, x in ((gk, k), (gv, v)):
+        _same(got[32:96], O.packed_values(W.bf16_bits_to_f64(x[64:128]), bits), "copied rows")
+        assert np.isnan(got[:32]).all() and np.isnan(got[96:]).all()
+
+
 def _rope_bound(want, d, style):
     a = np.abs(want)
     if style == 0:
