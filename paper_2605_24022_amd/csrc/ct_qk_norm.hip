@@ -52,14 +52,28 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(QkNormArgs a, Ro
   const bool is_q = head < a.Hq;
   const uint16_t* w = is_q ? a.q_weight : a.k_weight;
   const u32x4 wa = *reinterpret_cast<const u32x4*>(w + d_a), wb = *reinterpret_cast<const u32x4*>(w + d_b);
-  float fa[8], fb[8], ss = 0.f;
+  float fa[8], fb[8];
   widen8(xa, fa);
   widen8(xb, fb);
+  auto sum_squares = [&]() __attribute__((always_inline)) {
+    float t = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) ss += fa[i] * fa[i] + fb[i] * fb[i];
+    for (int i = 0; i < 8; ++i) t += fa[i] * fa[i] + fb[i] * fb[i];
 #pragma unroll
-  for (int off = THREADS / 2; off >= 1; off >>= 1) ss += __shfl_xor(ss, off);   // (the lanes of a head leave together)
-  const float inv = 1.0f / sqrtf(ss / (float)D + a.eps);
+    for (int off = THREADS / 2; off >= 1; off >>= 1) t += __shfl_xor(t, off);   // (the lanes of a head leave together)
+    return t;
+  };
+  float ss = sum_squares(), ms = ss / (float)D + a.eps;
+  if (!(ss <= 0x1p120f) || ms < 0x1p-80f) {   // squares that leave fp32: the same with elements and root scaled by 2^k
+    const float up = ss <= 0x1p120f ? 0x1p96f : 0x1p-70f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      fa[i] *= up;
+      fb[i] *= up;
+    }
+    ms = sum_squares() / (float)D + a.eps * up * up;
+  }
+  const float inv = 1.0f / sqrtf(ms);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     fa[2 * i] *= inv * bf16_lo(wa[i]);

@@ -428,6 +428,27 @@ def test_norm_and_rotation(hq, hkv, d, n, style, eps):
     assert np.array_equal(bits_of(q2)[:n], bits_of(q)[:n]) and np.array_equal(bits_of(k2)[:n], bits_of(k)[:n])
 
 
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("d", [64, 128])
+def test_norm_of_heads_whose_squares_leave_single_precision(eps, d):
+    """Heads of every size that bf16 holds: the norm brings them all to the size of the weights (eps permitting)."""
+    hq, hkv = 8, 2
+    say(f"qk norm sizes d={d} eps={eps}")
+    rng = np.random.default_rng(d)
+    x = rng.standard_normal((5, hq + 2 * hkv, d)) * 2.0 ** np.linspace(-120, 124, 12)[None, :, None]
+    x = W.f32_to_bf16_bits(x.astype(np.float32))
+    w = W.f32_to_bf16_bits((1 + 0.3 * rng.standard_normal(d)).astype(np.float32))
+    pos = np.array([0, 1, 77, 4096, 100000], dtype=np.int32)
+    q, k, v = (torch.empty((5, h, d), dtype=torch.bfloat16, device="cuda") for h in (hq, hkv, hkv))
+    B.ct_qk_norm_rope(_cfg(hq, hkv, d, 5e5), dev_bf16(x.reshape(5, -1)), dev_i32(pos), 5, dev_bf16(w), dev_bf16(w), eps, q, k, v)
+    wf = W.bf16_bits_to_f64(w)
+    want = O.qk_norm_rope(W.bf16_bits_to_f64(x).reshape(5, -1), pos, wf, wf, np.float32(eps), hq, hkv, d, 5e5)
+    for got, r in ((q, want[0]), (k, want[1])):
+        # 2^-133: the step of bf16 below its normal numbers
+        assert (np.abs(f64_of(got) - r) <= _rope_bound(r, d, 0) + 2.0 ** -18 * np.abs(r) + 2.0 ** -133).all()
+    _same(f64_of(v), want[2], "v")
+
+
 def test_norm_of_zeros_and_of_what_is_not_finite():
     """A head of zeros stays zero; NaN and infinities stay in their head."""
     hq, hkv, d = 4, 2, 64
