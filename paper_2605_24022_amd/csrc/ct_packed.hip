@@ -25,9 +25,11 @@ struct PackArgs {
 };
 
 // A workgroup takes 32 tokens of one head (those of one block of the cache, where the rows are a run), so that every
-// line of codes is written by one workgroup in whole (a thread per 8 elements in the order of the rows, whose lines several
-// dies write in parts: 32768 tokens and back 80 us instead of 71).  A thread takes 8 elements at a time; threads lie along the row for K and along the tokens for V, which is the
-// order of their codes; the threads that share a scale are 1, 2 and 3 (K) or 8, 16 and 24 (V) apart.
+// line of codes is written by one workgroup in whole (a thread per 8 elements in the order of the rows, whose lines
+// several dies write in parts: 32768 tokens and back 80 us instead of 71).  A thread takes 8 elements at a time; threads
+// lie along the row for K and along the tokens for V, which is the order of their codes; the threads that share a scale
+// are 1, 2 and 3 (K) or 8, 16 and 24 (V) apart.  A row's number comes before its elements are sent for (both at once:
+// 0.3 us less for 48 tokens, but 63 us instead of 59 for 32768 and back).
 template <int D, int BITS>
 __global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
   using L = PackLayout<D, BITS>;

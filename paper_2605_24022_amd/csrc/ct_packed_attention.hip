@@ -125,12 +125,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
   const int lane = threadIdx.x & 63, l16 = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const int g = blockIdx.x % a.Hkv;
-  int rest = blockIdx.x / a.Hkv;
-  const int cb = rest % a.col_blocks;
-  rest /= a.col_blocks;
-  const int part = rest % a.n_parts;
-  const int b = rest / a.n_parts;
+  uint32_t rest = blockIdx.x;
+  auto next_of = [&](uint32_t n) __attribute__((always_inline)) {
+    const uint32_t q = rest / n, r = rest - q * n;
+    rest = q;
+    return (int)r;
+  };
+  const int g = next_of(a.Hkv), cb = next_of(a.col_blocks), part = next_of(a.n_parts), b = (int)rest;
   const Sequence seq = sequence_of(a, b);
   if (part >= max(seq.n_parts, 1)) return;            // (an empty sequence still gets its zeros, from part 0)
 
@@ -423,9 +424,8 @@ __global__ __launch_bounds__(kMergeThreads) void packed_merge_kernel(PackedAttnA
   const int tid = threadIdx.x;
   const int G = 1 << a.group_shift, n_cols = a.n_new << a.group_shift;
   const int64_t row = blockIdx.x;                       // (sequence, new token, query head)
-  const int hq = (int)(row % a.Hq);
-  const int64_t bt = row / a.Hq;
-  const int t = (int)(bt % a.n_new), b = (int)(bt / a.n_new);
+  const uint32_t bt = blockIdx.x / (uint32_t)a.Hq, n_new = a.n_new;   // (in 32 bits: a division in 64 is some 100 steps)
+  const int hq = blockIdx.x - bt * (uint32_t)a.Hq, b = bt / n_new, t = bt - (uint32_t)b * n_new;
   const int np = sequence_of(a, b).n_parts;
   if (np <= 1) return;                                  // written by the attention kernel
   const int col = (t << a.group_shift) + (hq & (G - 1));

@@ -34,24 +34,25 @@ struct QkNormArgs {
 template <int D, int STYLE>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(QkNormArgs a, RopeTable table) {
   constexpr int THREADS = D / 16;
-  const int64_t gid = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int jg = (int)(gid % THREADS);
-  const int64_t rest = gid / THREADS;
-  const int head = (int)(rest % a.heads);
-  const int64_t t = rest / a.heads;
+  const uint32_t gid = blockIdx.x * kThreads + threadIdx.x, rest = gid / THREADS, n_heads = a.heads;   // (below 2^32 threads)
+  const int jg = gid % THREADS;
+  const int64_t t = rest / n_heads;
+  const int head = rest - (uint32_t)t * n_heads;
   if (t >= a.n_tokens) return;
   const int d_a = piece_a<D>(jg), d_b = piece_b<D>(jg);
   const uint16_t* src = a.qkv + (t * (a.Hq + 2 * a.Hkv) + head) * D;
+  // everything that is read is sent for at once: with few rows the latency counts
   const u32x4 xa = *reinterpret_cast<const u32x4*>(src + d_a), xb = *reinterpret_cast<const u32x4*>(src + d_b);
+  const bool is_q = head < a.Hq;
+  const uint16_t* w = is_q ? a.q_weight : a.k_weight;
+  const u32x4 wa = *reinterpret_cast<const u32x4*>(w + d_a), wb = *reinterpret_cast<const u32x4*>(w + d_b);
+  const int32_t pos = a.pos[t];
   if (head >= a.Hq + a.Hkv) {
     uint16_t* dst = a.v + (t * a.Hkv + head - a.Hq - a.Hkv) * D;
     __builtin_nontemporal_store(xa, reinterpret_cast<u32x4*>(dst + d_a));
     __builtin_nontemporal_store(xb, reinterpret_cast<u32x4*>(dst + d_b));
     return;
   }
-  const bool is_q = head < a.Hq;
-  const uint16_t* w = is_q ? a.q_weight : a.k_weight;
-  const u32x4 wa = *reinterpret_cast<const u32x4*>(w + d_a), wb = *reinterpret_cast<const u32x4*>(w + d_b);
   float fa[8], fb[8];
   widen8(xa, fa);
   widen8(xb, fb);
@@ -81,7 +82,6 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(QkNormArgs a, Ro
     fb[2 * i] *= inv * bf16_lo(wb[i]);
     fb[2 * i + 1] *= inv * bf16_hi(wb[i]);
   }
-  const int32_t pos = a.pos[t];
   float cs[8], sn[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) sincos_turns(pos, table.turns[pair_of<D, STYLE>(jg, i)], cs[i], sn[i]);
