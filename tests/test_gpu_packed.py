@@ -318,6 +318,35 @@ def test_many_sequences():
     _check_attention(8, 2, 64, 4, 1, lens, starts, (sum(lens) + 31) // 32 * 32)
 
 
+@pytest.mark.parametrize("n_seq", [17, 32, 33, 64, 65, 200, 256, 257])
+def test_batches_in_the_order_of_their_lengths(n_seq):
+    """Long batches take their sequences in another order than they come, 16 of them do not: every sequence gets the same bits."""
+    hq, hkv, d, n_rows, max_len = 16, 16, 64, 4096, 2100
+    say(f"order of lengths n_seq={n_seq}")
+    rng = np.random.default_rng(n_seq)
+    cfg = _cfg(hq, hkv, d)
+    cache = _cache(cfg, n_rows, 4)
+    _pack(cfg, _bits(rng, n_rows, hkv, d, spread=0.3), _bits(rng, n_rows, hkv, d, spread=0.3), cache, n_rows, 4)
+    q = dev_bf16(_bits(rng, n_seq, 1, hq, d, spread=0.3))
+    # many of equal length, empty ones, some at and beyond the bound, one below zero, one whose start is no row
+    lens = rng.choice([0, 1, 31, 32, 33, 70, 500, 1999, 2100], n_seq)
+    lens[[2, 5, 11]] = 5000, -7, 64
+    starts = rng.integers(0, n_rows - max_len, n_seq)
+    starts[11] = n_rows
+    got = torch.full_like(q, float("nan"))
+    _attend(cfg, q, n_seq, 1, cache, n_rows, 4, starts, lens, max_len, got)
+    want = torch.full_like(q, float("nan"))
+    for b in range(0, n_seq, 16):
+        b = min(b, n_seq - 16)
+        e = b + 16
+        _attend(cfg, q[b:e], e - b, 1, cache, n_rows, 4, starts[b:e], lens[b:e], max_len, want[b:e])
+    torch.cuda.synchronize()
+    assert not torch.isnan(got).any()
+    got, want = bits_of(got), bits_of(want)
+    bad = [b for b in range(n_seq) if not np.array_equal(got[b], want[b])]
+    assert not bad, f"sequences {bad[:8]} of lengths {lens[bad[:8]]} differ"
+
+
 def test_sequences_may_share_rows():
     """Two requests over one prompt: overlapping ranges of the cache."""
     _check_attention(16, 8, 128, 4, 1, [500, 500, 200], [10, 10, 300], 512)
