@@ -555,6 +555,10 @@ struct PackedPlan {
 // 83.6 / 85.3; but eight of 4096 to 16384 rows with four tokens 29.7 / 26.9.  768 are slower throughout (64 sequences of
 // 4096 rows 46 us with 512, 52 with 768): three workgroups fit a unit, and beyond them a second round starts that does
 // not fill.
+// More whole sequences than units are not divided in two: taken by length they share the units well, and no merge is needed
+// (uneven lengths, divided / whole: 36 sequences up to 4099 rows 29.9 / 25.2 us, 56 38.3 / 30.0, 60 up to 16384 134 / 111, in 8
+// bits 252 / 219), except long ones that leave more than half of the units with one workgroup alone (33 of 16384 rows 80.4
+// / 84.1, in 8 bits 162 / 163 and 153 / 179 where all are as long; 48 99.2 / 96.9 and 192 / 190).
 PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, int64_t max_len) {
   PackedPlan p;
   const int64_t n_cols = n_new * (cfg->n_q_heads / cfg->n_kv_heads);
@@ -567,7 +571,8 @@ PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, in
     return (blocks + parts - 1) / parts;
   };
   int64_t per = blocks_per(kNumCUs);
-  if (per > 128) per = blocks_per(2 * kNumCUs);
+  const bool whole = groups > kNumCUs && (blocks <= 257 || 2 * groups >= 3 * kNumCUs);
+  if (per > 128 && !whole) per = blocks_per(2 * kNumCUs);
   if (per < 4) per = 4;
   if (blocks * p.col_tiles <= 33) per = blocks;
   p.part_blocks = (int)per;
