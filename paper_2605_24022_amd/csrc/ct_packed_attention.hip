@@ -23,7 +23,7 @@ namespace ct {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kMaxParts = 2 * kNumCUs;
+constexpr int kMaxParts = 3 * kNumCUs;
 constexpr int kOrdered = 256;      // sequences that are taken in the order of their lengths
 
 struct PackedAttnArgs {
@@ -552,9 +552,11 @@ struct PackedPlan {
 // parts would be longer than 4096 rows, until two do, because sequences of uneven length leave units idle for as long
 // as a part takes.  256 / 512 workgroups, 32/8 heads of 128, 4 bits, one token: one sequence of 8192 rows 10.4 / 10.5 us,
 // of 32768 13.0 / 14.6, of 65536 18.1 / 19.8; four of 8192 12.8 / 13.5, of 32768 28.3 / 29.0, two of 131072 in 8 bits
-// 83.6 / 85.3; but eight of 4096 to 16384 rows with four tokens 29.7 / 26.9.  768 are slower throughout (64 sequences of
-// 4096 rows 46 us with 512, 52 with 768): three workgroups fit a unit, and beyond them a second round starts that does
-// not fill.
+// 83.6 / 85.3; but eight of 4096 to 16384 rows with four tokens 29.7 / 26.9.  Never a few more than fit, and two or three to
+// a unit where fewer would leave places empty (as many parts as reach 256 or 512 workgroups / this rule: 5 sequences of
+// 65536 rows 71.8 / 57.7 us, 9 of up to 4099 14.1 / 12.4, 12 16.8 / 13.8, in 8 bits 25.9 / 20.9, 24 of up to 8192 36.3 / 31.5;
+// the worst, 13 of up to 16384, 32.5 / 35.5).  Three fit a unit, and are slower where two fill it (64 sequences of 4096 rows
+// 46 us with 512 workgroups, 52 with 768).
 // More whole sequences than units are not divided in two: taken by length they share the units well, and no merge is needed
 // (uneven lengths, divided / whole: 36 sequences up to 4099 rows 29.9 / 25.2 us, 56 38.3 / 30.0, 60 up to 16384 134 / 111, in 8
 // bits 252 / 219), except long ones that leave more than half of the units with one workgroup alone (33 of 16384 rows 80.4
@@ -566,13 +568,19 @@ PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, in
   p.col_blocks = (int)((n_cols + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
   const int64_t blocks = (max_len + kPackRows - 1) / kPackRows + 1;   // a sequence may start inside a block
   const int64_t groups = n_seq * cfg->n_kv_heads * p.col_blocks;
-  auto blocks_per = [&](int64_t workgroups) {
-    const int64_t parts = (workgroups + groups - 1) / groups;
-    return (blocks + parts - 1) / parts;
-  };
-  int64_t per = blocks_per(kNumCUs);
-  const bool whole = groups > kNumCUs && (blocks <= 257 || 2 * groups >= 3 * kNumCUs);
-  if (per > 128 && !whole) per = blocks_per(2 * kNumCUs);
+  int64_t parts[4], used[4];      // where k workgroups stand on a unit: parts of a sequence, sixteenths of the places that are taken
+  for (int k = 1; k <= 3; ++k) {
+    parts[k] = std::max<int64_t>(k * kNumCUs / groups, 1);
+    used[k] = 16 * groups * parts[k] / (k * kNumCUs);
+  }
+  auto blocks_per = [&](int k) { return (blocks + parts[k] - 1) / parts[k]; };
+  int64_t per = blocks_per(1);
+  if (groups <= kNumCUs || (blocks > 257 && 2 * groups < 3 * kNumCUs)) {
+    int k = per > 128 ? 2 : 1;
+    const int64_t most = std::max({used[1], used[2], used[3]});
+    while (k < 3 && used[k] < most - 1) ++k;
+    per = blocks_per(k);
+  }
   if (per < 4) per = 4;
   if (blocks * p.col_tiles <= 33) per = blocks;
   p.part_blocks = (int)per;
