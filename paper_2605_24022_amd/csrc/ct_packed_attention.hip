@@ -569,7 +569,8 @@ PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, in
   const int64_t blocks = (max_len + kPackRows - 1) / kPackRows + 1;   // a sequence may start inside a block
   const int64_t groups = n_seq * cfg->n_kv_heads * p.col_blocks;
   int64_t parts[4], used[4];      // where k workgroups stand on a unit: parts of a sequence, sixteenths of the places that are taken
-  for (int k = 1; k <= 3; ++k) {
+  const int fit = p.col_tiles == 1 ? 3 : 2;      // workgroups that a unit holds
+  for (int k = 1; k <= fit; ++k) {
     parts[k] = std::max<int64_t>(k * kNumCUs / groups, 1);
     used[k] = 16 * groups * parts[k] / (k * kNumCUs);
   }
@@ -577,8 +578,8 @@ PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, in
   int64_t per = blocks_per(1);
   if (groups <= kNumCUs || (blocks > 257 && 2 * groups < 3 * kNumCUs)) {
     int k = per > 128 ? 2 : 1;
-    const int64_t most = std::max({used[1], used[2], used[3]});
-    while (k < 3 && used[k] < most - 1) ++k;
+    const int64_t most = *std::max_element(used + 1, used + fit + 1);
+    while (k < fit && used[k] < most - 1) ++k;
     per = blocks_per(k);
   }
   if (per < 4) per = 4;
