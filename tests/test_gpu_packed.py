@@ -312,6 +312,14 @@ def test_bound_above_the_lengths():
     _check_attention(32, 8, 128, 4, 2, [100, 900, 0], [40, 200, 0], 32768, max_len=30000)
 
 
+@pytest.mark.parametrize("n_seq", [3, 5, 7, 9, 11, 13, 17, 20, 24, 31, 33, 47, 49])
+@pytest.mark.parametrize("bits,n_new", [(4, 1), (8, 20)])
+def test_batches_divided_one_two_and_three_to_a_unit(n_seq, bits, n_new):
+    lens = [1500 - 211 * i % 1400 for i in range(n_seq)]
+    starts = np.concatenate([[0], np.cumsum(lens)[:-1]]).tolist()
+    _check_attention(8, 8, 64, bits, n_new, lens, starts, (sum(lens) + 31) // 32 * 32)
+
+
 def test_many_sequences():
     lens = [(37 * i) % 150 for i in range(300)]
     starts = np.concatenate([[0], np.cumsum(lens)[:-1]]).tolist()
