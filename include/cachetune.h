@@ -447,7 +447,8 @@ ct_status ct_unpack_kv(const ct_layer_cfg* cfg, const void* cache, int32_t n_row
  *   max_len    host bound of the lengths, at most n_rows; the key range is divided over workgroups for this length
  *   lse        device fp32 [n_seq, n_new, n_q_heads] natural-log sum-exp of the scaled scores, or NULL
  *   workspace  device scratch of at least ct_packed_attention_workspace_bytes() bytes, 256-byte aligned (none where
- *              that is 0); calls that overlap in time need one each
+ *              that is 0); calls that overlap in time need one each.  Fewer or shorter sequences may need more of
+ *              it; 65536 * (head_dim + 2) bytes are enough for every call
  * The result of a call does not depend on what else runs; it depends on max_len, n_seq and n_new in the order of its
  * fp32 sums.  n_seq = 0 is legal and does nothing. */
 ct_status ct_packed_attention(const ct_layer_cfg* cfg, const void* q, int32_t n_seq, int32_t n_new, const void* cache,

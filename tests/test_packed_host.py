@@ -190,3 +190,13 @@ def test_qk_norm_refusals():
     for name in ("qkv", "qw", "kw", "q", "k", "v"):
         assert call(**{name: FAKE + 2}) == B.CT_ERR_UNSUPPORTED
     B.ct_qk_norm_rope(c, None, None, 0, None, None, 1e-6, None, None, None)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (32, 8, 128), (16, 1, 128), (16, 16, 64), (2, 1, 64), (64, 8, 128)])
+def test_one_workspace_is_enough_for_attention_of_every_size(hq, hkv, d):
+    cfg = B.make_cfg(hq * d, hq, hkv, d, 1e4, 0, 0.0)
+    for n_new in (1, 2, 4, 5, 8, 9, 17, 33, 64):
+        for n_seq in [*range(1, 66), 100, 128, 200, 255, 256, 257, 300, 1000]:
+            for max_len in (0, 1, 1024, 1025, 2049, 4099, 8192, 8225, 65536, 1 << 20, 1 << 30):
+                need = B.ct_packed_attention_workspace_bytes(cfg, n_seq, n_new, max_len)
+                assert 0 <= need <= 65536 * (d + 2), (n_seq, n_new, max_len, need)
