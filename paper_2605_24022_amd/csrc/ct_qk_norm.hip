@@ -3,7 +3,7 @@
 //
 //   y = x / sqrt(mean(x^2) + eps) * w over the D elements of a head, then RoPE at the token's position; v is copied.
 // fp32 from the bf16 input to the one rounding of the result.  Bound: memory, each element read and written once: 4915
-// rows of 32 + 8 + 8 heads of 128, 121 MB, 23.7 us (5.1 TB/s, what a large copy reaches); 7 rows 4.9 us, the launch.
+// rows of 32 + 8 + 8 heads of 128, 121 MB, 22.2 us (5.5 TB/s; a large copy reaches 5.1); 7 rows 4.6 us, the launch.
 #include <math.h>
 
 #include "ct_internal.h"
