@@ -327,7 +327,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
             for (int i = 0; i < 4; ++i) o[m][n][i] *= alpha;
         }
     }
-    bf16x8 pf[NT];
+    bf16x8 pf[NT], pl[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float m_use = m_run[n] == -INFINITY ? 0.f : m_run[n];
@@ -335,10 +335,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][n][i % 4], a.scale_log2, -m_use));
       l_run[n] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-      // bf16 operands: off by up to half a step, 2^-8 of a probability, independently from key to key; the sum above is
-      // unrounded.  (A second product for what the rounding leaves: 3 to 6 % slower, 10 % with 8-bit codes.)
+      // bf16 operands: a probability is the sum of two, its rounding and the rounding of what that leaves, which is off by
+      // up to 2^-16 of it; the sum above is unrounded.  (The first alone is off by up to 2^-8: outputs 0.0023 from the exact
+      // ones in relative 2-norm, where their own rounding makes 0.0017.  The second product costs 0 to 2 % where memory
+      // decides (64 uneven sequences up to 4099 rows 33.1 -> 33.4 us, 2 of 131072 in 8 bits 85.0 -> 85.2), 7 % of one
+      // sequence of 1024 rows with heads of 64 (5.35 -> 5.74) and up to 18 % where the vector and matrix units do: 16
+      // sequences of 8192 rows with 64 columns 58 -> 68, in 8 bits 75.5 -> 80.)
       const u32x4 w = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
       pf[n] = __builtin_bit_cast(bf16x8, w);
+      u32x4 rest;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rest[i] = pack_bf16(p[2 * i] - bf16_lo(w[i]), p[2 * i + 1] - bf16_hi(w[i]));
+      pl[n] = __builtin_bit_cast(bf16x8, rest);
     }
     // O^T += V^T P^T
     float v_scale[8];
@@ -363,6 +371,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
       for (int n = 0; n < NT; ++n) {
         o[2 * E2][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pf[n], o[2 * E2][n], 0, 0, 0);
         o[2 * E2 + 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pf[n], o[2 * E2 + 1][n], 0, 0, 0);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        o[2 * E2][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pl[n], o[2 * E2][n], 0, 0, 0);
+        o[2 * E2 + 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pl[n], o[2 * E2 + 1][n], 0, 0, 0);
       }
     });
   };
