@@ -75,12 +75,13 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(QkNormArgs a, Ro
     ms = sum_squares() / (float)D + a.eps * up * up;
   }
   const float inv = 1.0f / sqrtf(ms);
+  // (the element by the root first, then by the weight: no size of a head leaves fp32 beside any weight)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    fa[2 * i] *= inv * bf16_lo(wa[i]);
-    fa[2 * i + 1] *= inv * bf16_hi(wa[i]);
-    fb[2 * i] *= inv * bf16_lo(wb[i]);
-    fb[2 * i + 1] *= inv * bf16_hi(wb[i]);
+    fa[2 * i] = fa[2 * i] * inv * bf16_lo(wa[i]);
+    fa[2 * i + 1] = fa[2 * i + 1] * inv * bf16_hi(wa[i]);
+    fb[2 * i] = fb[2 * i] * inv * bf16_lo(wb[i]);
+    fb[2 * i + 1] = fb[2 * i + 1] * inv * bf16_hi(wb[i]);
   }
   float cs[8], sn[8];
 #pragma unroll
