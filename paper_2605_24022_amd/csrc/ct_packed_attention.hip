@@ -25,6 +25,11 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kMaxParts = 3 * kNumCUs;
 constexpr int kOrdered = 256;      // sequences that are taken in the order of their lengths
+// Probabilities are held as 2^-kLift of what they are, in reach of the largest values and of the smallest: sums over 2^19
+// rows of up to 2^kLag * 1.75 * 2^127 stay below 2^128 (a sum that does not is an infinity, which no weight of zero
+// silences when waves are joined), and a product with the smallest value of a cache, 2^-126, is still one of fp32's.
+constexpr float kLift = 23.f;
+constexpr float kLag = 4.f;        // binary orders by which a maximum may exceed the reference of the exponents
 
 struct PackedAttnArgs {
   const uint16_t* q;              // [n_seq, n_new, Hq, D]
@@ -219,7 +224,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
   // ---- state -----------------------------------------------------------------------------------------
   f32x4 o[MT][NT];
   float m_run[NT], m_limit[NT], l_run[NT];
-  const float limit_step = 8.0f / a.scale_log2;
+  const float limit_step = kLag / a.scale_log2;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     m_run[n] = m_limit[n] = -INFINITY;
@@ -299,7 +304,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
       }
     }
     // Online softmax.  The reference of the exponents follows the running maximum lazily: it moves when a score exceeds
-    // it by more than 2^8, so probabilities stay below 256 and rescaling is rare.
+    // it by more than 2^kLag, so rescaling is rare.  (2^8 instead of 2^4: within 0.5 %.)
     float mx[NT];
     bool moves = false;
 #pragma unroll
@@ -316,7 +321,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
 #pragma unroll
       for (int n = 0; n < NT; ++n)
         if (mx[n] > m_limit[n]) {
-          const float m_new = mx[n] * a.scale_log2;
+          const float m_new = mx[n] * a.scale_log2 + kLift;
           const float alpha = __builtin_amdgcn_exp2f(m_run[n] - m_new);   // (0 from the first reference on)
           m_run[n] = m_new;
           m_limit[n] = mx[n] + limit_step;

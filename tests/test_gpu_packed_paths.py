@@ -29,8 +29,9 @@ def _rows(rng, *shape):
     return W.f32_to_bf16_bits(rng.standard_normal(shape).astype(np.float32))
 
 
-def _definition(q, k, v, scale):
-    """One sequence: outputs [n_new, Hq, D], log-sum-exp, and how far from them the kernel may be."""
+def _definition(q, k, v, scale, floor=0.0):
+    """One sequence: outputs [n_new, Hq, D], log-sum-exp, and how far from them the kernel may be (floor: see where it is
+    given)."""
     n_new, hq, d = q.shape
     n, hkv, _ = k.shape
     out, off = np.zeros((n_new, hq, d)), np.zeros((n_new, hq, d))
@@ -46,14 +47,15 @@ def _definition(q, k, v, scale):
             p = w / w.sum()
             o = p @ vg
             e = d * 2.0 ** -24 * (np.abs(kg) @ np.abs(q[t, h])) * scale + 2.0 ** -22 * (np.abs(s) + abs(s.max())) + 2.0 ** -20
-            slack = (p * e) @ (np.abs(vg) + np.abs(o)) + (2.0 ** -16 + 2.0 ** -18) * (p @ np.abs(vg))
+            slack = (p * e) @ (np.abs(vg) + np.abs(o)) + (2.0 ** -16 + 2.0 ** -18) * (p @ np.abs(vg)) + floor * seen / w.sum()
             out[t, h], off[t, h] = o, 2.0 ** -8 * (np.abs(o) + slack) + slack
             lse[t, h] = s.max() + np.log(w.sum())
             lse_off[t, h] = p @ e + 2.0 ** -18 + 2.0 ** -22 * abs(lse[t, h])
     return out, off, lse, lse_off
 
 
-def _check(hq, hkv, d, bits, n_new, lens, starts, n_rows, max_len=None, divided=None, by_length=None, streamed=None):
+def _check(hq, hkv, d, bits, n_new, lens, starts, n_rows, max_len=None, divided=None, by_length=None, streamed=None,
+           values=_rows, queries=_rows, floor=0.0):
     """The call against the definition; rows outside the sequences read as NaN.  What the case is there for is held to the
     rules of the host: `divided`, the key range of max_len rows (which the workspace shows); `by_length`, whole sequences
     on more than 256 workgroups; `streamed`, 8-bit codes on one workgroup for all columns, rows enough for all sequences."""
@@ -72,7 +74,7 @@ def _check(hq, hkv, d, bits, n_new, lens, starts, n_rows, max_len=None, divided=
         assert (bits == 4 or (cols <= 32 and n_seq * max_len <= n_rows)) == streamed
     cache = torch.full((B.ct_packed_kv_bytes(cfg, n_rows, bits),), 0xff, dtype=torch.uint8, device="cuda")
     rows = np.unique(np.concatenate([np.arange(s, s + n) for s, n in zip(starts, lens)])).astype(np.int32)
-    k, v, q = _rows(rng, rows.size, hkv, d), _rows(rng, rows.size, hkv, d), _rows(rng, n_seq, n_new, hq, d)
+    k, v, q = _rows(rng, rows.size, hkv, d), values(rng, rows.size, hkv, d), queries(rng, n_seq, n_new, hq, d)
     kd, vd = dev_bf16(k), dev_bf16(v)
     B.ct_pack_kv(cfg, kd, hkv * d, vd, hkv * d, rows.size, dev_i32(rows), 0, cache, n_rows, bits)
     out = torch.full((n_seq, n_new, hq, d), float("nan"), dtype=torch.bfloat16, device="cuda")
@@ -84,7 +86,7 @@ def _check(hq, hkv, d, bits, n_new, lens, starts, n_rows, max_len=None, divided=
     qv = W.bf16_bits_to_f64(q)
     for b, (s, n) in enumerate(zip(starts, lens)):
         at = np.searchsorted(rows, s)
-        want, off, want_lse, lse_off = _definition(qv[b], kv[at:at + n], vv[at:at + n], d ** -0.5)
+        want, off, want_lse, lse_off = _definition(qv[b], kv[at:at + n], vv[at:at + n], d ** -0.5, floor)
         beyond = np.abs(got[b] - want) - off
         assert not (beyond > 0).any() and not np.isnan(got[b]).any(), \
             f"sequence {b}: {(beyond > 0).sum()} of {beyond.size} outputs beyond their bound, by up to {np.nanmax(beyond / np.maximum(off, 1e-30))} of it"
@@ -169,3 +171,30 @@ def test_infinities_and_nan_among_many_columns(hq, hkv, d, bits, n_new, bad):
         v[600 + 3, 1, 40] = bad           # an early row of sequence 2: everybody sees it
         v[15], k[15], v[397], k[396] = bad, bad, bad, bad
     _check_attention(hq, hkv, d, bits, n_new, [301, 71, 50, 3], [16, 400, 600, 394], 704, edit=edit)
+
+
+# ---------------------------------------------------------------------------------- values at the ends of the range
+def _of_exponents(lo, hi):
+    """bf16 patterns of any sign and mantissa up to 1.75, exponents lo to hi."""
+    def rows(rng, *shape):
+        return (rng.integers(0, 2, shape) << 15 | rng.integers(lo, hi + 1, shape) << 7 | rng.integers(0, 0x61, shape)).astype(np.uint16)
+    return rows
+
+
+@pytest.mark.parametrize("hq,hkv,d,n_new", [(8, 2, 64, 1), (32, 8, 128, 1), (32, 8, 128, 5)])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("lens", [[700, 33, 1], [5000, 70]])
+def test_sums_of_the_largest_values_stay_finite(hq, hkv, d, n_new, bits, lens):
+    """Values from 2^126 to 1.75 * 2^127: their average is one of them, their sum is not in fp32.  (A weight of zero for what
+    another wave or part has summed up silences a sum, but not an infinity.)"""
+    starts = [5, 5 + lens[0], 5 + sum(lens[:2])][:len(lens)]
+    _check(hq, hkv, d, bits, n_new, lens, starts, 5120, values=_of_exponents(253, 254))
+
+
+@pytest.mark.parametrize("hq,hkv,d,n_new", [(8, 2, 64, 1), (32, 8, 128, 5)])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_the_smallest_values_keep_their_bits(hq, hkv, d, n_new, bits):
+    """Values from 2^-126 up.  floor: products and sums are held as 2^-23 of themselves in steps of 2^-149 and off by less
+    than one of them, at most three a row (two products, one sum), over a sum of weights of sum_j w_j or more."""
+    _check(hq, hkv, d, bits, n_new, [300, 33, 1], [5, 305, 338], 352, values=_of_exponents(1, 18),
+           queries=lambda rng, *shape: W.f32_to_bf16_bits((0.05 * rng.standard_normal(shape)).astype(np.float32)), floor=3 * 2.0 ** (23 - 149))
