@@ -1,4 +1,5 @@
-"""The scales that the attention over packed caches reads beside one another, against the oracle."""
+"""The values that a packed cache stands for, over all bf16 numbers: rows written and read back bit for bit, and the scales
+that the attention reads beside one another, against the oracle."""
 import numpy as np
 import pytest
 import torch
@@ -16,6 +17,61 @@ def _need_gpu():
     assert torch.cuda.is_available()
     B.load()
     torch.cuda.set_device(0)
+
+
+MANTISSAS = np.array([0x00, 0x5f, 0x60, 0x61, 0x7f])      # both sides of 1.75, where the scale changes, and the ends
+
+
+def _there_and_back(groups, d, bits):
+    """Groups [n, 32] of bf16 patterns as the K rows of one head, and in the opposite order as its V rows."""
+    per_row = d // 32
+    n = -(-groups.shape[0] // (32 * per_row)) * 32
+    x = np.zeros((n * per_row, 32), dtype=np.uint16)
+    x[: groups.shape[0]] = groups
+    x = x.reshape(n, 1, d)
+    cfg = B.make_cfg(64 * d, 1, 1, d, 1e4, 0, 0.0)
+    cache = torch.full((B.ct_packed_kv_bytes(cfg, n, bits),), 0xff, dtype=torch.uint8, device="cuda")
+    B.ct_pack_kv(cfg, dev_bf16(x), d, dev_bf16(x[::-1]), d, n, None, 0, cache, n, bits)
+    k, v = (torch.full((n, 1, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.ct_unpack_kv(cfg, cache, n, bits, None, 0, None, None, n, k, v)
+    want = O.packed_values(W.bf16_bits_to_f64(x), bits)
+    for name, got in (("K", f64_of(k)), ("V", f64_of(v)[::-1])):
+        bad = got != want
+        assert not bad.any(), f"{name}: {bad.sum()} of {bad.size} differ, first {got[bad][0]} for {want[bad][0]}"
+
+
+def _in_groups(tops, elements):
+    """31 elements a group behind its largest one; elements above it become it."""
+    e = np.concatenate([elements, elements[: -elements.size % 31]]).reshape(-1, 31)
+    out = np.empty((tops.size, e.shape[0], 32), dtype=np.uint16)
+    out[:, :, 0] = tops[:, None]
+    out[:, :, 1:] = np.where((e & 0x7fff)[None] <= tops[:, None, None], e[None], tops[:, None, None])
+    return out.reshape(-1, 32)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("exponents", [(0, 8, 9, 10), (12, 100, 127, 128), (200, 252, 253, 254)])
+def test_all_finite_numbers_beside_borders_of_some_scales(d, bits, exponents):
+    say(f"packed values, all finite ones, d={d} bits={bits} exponents={exponents}")
+    every = np.arange(65536, dtype=np.uint32).astype(np.uint16)
+    every = every[(every & 0x7f80) != 0x7f80]
+    tops = ((np.array(exponents)[:, None] << 7) | MANTISSAS[None]).ravel().astype(np.uint16)
+    _there_and_back(_in_groups(tops, every), d, bits)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_numbers_that_count_beside_borders_of_all_scales(d, bits):
+    """Every exponent of the largest magnitude, both sides of the border, with all numbers down to those that become zero."""
+    reach = 6 if bits == 4 else 19
+    say(f"packed values, all scales, d={d} bits={bits}")
+    groups = []
+    for exp in range(255):
+        below = np.arange(max(exp - reach, 0) << 7, (exp + 1) << 7)
+        below = np.concatenate([below, below | 0x8000]).astype(np.uint16)
+        groups.append(_in_groups(((exp << 7) | MANTISSAS).astype(np.uint16), below))
+    _there_and_back(np.concatenate(groups), d, bits)
 
 
 @pytest.mark.parametrize("d", [64, 128])
