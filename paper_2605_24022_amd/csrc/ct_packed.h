@@ -34,7 +34,6 @@ struct PackLayout {
   static constexpr int kRowBytes = D * BITS / 8;               // codes of one K row
   static constexpr int kCodeBytes = kPackRows * kRowBytes;     // of one tensor, head and block
   static constexpr int kScaleBytes = D;                        // D / 32 groups x 32 rows
-  static constexpr int kGroups = D / kPackGroup;
   static constexpr int kVCodes = kCodeBytes, kKScales = 2 * kCodeBytes, kVScales = 2 * kCodeBytes + kScaleBytes;
   static constexpr int kBytes = 2 * (kCodeBytes + kScaleBytes);   // one head of one block
   static constexpr int kLaneDims = D / 16;                     // V dimensions per lane
@@ -42,7 +41,7 @@ struct PackLayout {
 
   // A lane's share of a K row or of V (16, 32 or 64 bytes, or 8) lies in quads of 16 bytes, the same quad of neighbouring
   // lanes side by side.
-  static constexpr int kShareK = kRowBytes / 4, kShareV = 8 * kLaneBytes;
+  static constexpr int kShareK = kRowBytes / 4;
   static __device__ __forceinline__ int k_code(int row, int dim) {
     const int byte = dim * BITS / 8, in = byte % kShareK;
     return row * kRowBytes + (kShareK <= 16 ? byte : in / 16 * 64 + byte / kShareK * 16 + in % 16);

@@ -587,10 +587,10 @@ PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, in
   const int64_t blocks = (max_len + kPackRows - 1) / kPackRows + 1;   // a sequence may start inside a block
   const int64_t groups = n_seq * cfg->n_kv_heads * p.col_blocks;
   int64_t parts[4], used[4];      // where k workgroups stand on a unit: parts of a sequence, sixteenths of the places that are taken
-  const int fit = p.col_tiles == 1 ? 3 : 2;      // workgroups that a unit holds
+  const int fit = p.col_tiles == 1 ? 3 : 2;      // what a unit holds with heads of 128 (4 and 3 with heads of 64)
   for (int k = 1; k <= fit; ++k) {
     parts[k] = std::max<int64_t>(k * kNumCUs / groups, 1);
-    used[k] = 16 * groups * parts[k] / (k * kNumCUs);
+    used[k] = std::min<int64_t>(16 * groups * parts[k] / (k * kNumCUs), 16);
   }
   auto blocks_per = [&](int k) { return (blocks + parts[k] - 1) / parts[k]; };
   int64_t per = blocks_per(1);
