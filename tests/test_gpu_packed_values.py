@@ -133,3 +133,39 @@ def test_scales_beside_any_others(d, bits):
     got = f64_of(out)[:, 0]
     bad = got != want
     assert not bad.any(), f"V: {bad.sum()} of {bad.size} differ, first {got[bad][0]} for {want[bad][0]}"
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("power", [8, 16, 24, 28])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_of_any_size(d, bits, power, sign):
+    """Scores of about 2^power of either sign: the key ahead of the others by half of that gets all the weight, its V row
+    comes out bit for bit, and the log-sum-exp is its score, off by a few fp32 roundings of it and of it times log2 e."""
+    hkv, n_seq, length = 2, 96, 200
+    say(f"packed scores of 2^{power} d={d} bits={bits} sign={sign}")
+    rng = np.random.default_rng([d, bits, power])
+    cfg = B.make_cfg(hkv * d, hkv, hkv, d, 1e4, 0, 1.0)
+    n_rows = n_seq * length // 32 * 32 + 32
+    ahead, behind = (1.5, 1.0) if sign > 0 else (-1.0, -1.5)        # exact in both formats, alone in their group
+    k = np.zeros((n_rows, hkv, d))
+    k[..., 37] = behind
+    best = rng.integers(0, length, (n_seq, hkv))
+    start = np.arange(n_seq) * length
+    for h in range(hkv):
+        k[start + best[:, h], h, 37] = ahead
+    q = np.zeros((n_seq, 1, hkv, d))
+    q[..., 37] = 2.0 ** power
+    v = rng.standard_normal((n_rows, hkv, d))
+    kb, vb, qb = (W.f32_to_bf16_bits(x.astype(np.float32)) for x in (k, v, q))
+    cache = torch.full((B.ct_packed_kv_bytes(cfg, n_rows, bits),), 0xff, dtype=torch.uint8, device="cuda")
+    B.ct_pack_kv(cfg, dev_bf16(kb), hkv * d, dev_bf16(vb), hkv * d, n_rows, None, 0, cache, n_rows, bits)
+    out = torch.full((n_seq, 1, hkv, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((n_seq, 1, hkv), float("nan"), device="cuda")
+    B.ct_packed_attention(cfg, dev_bf16(qb), n_seq, 1, cache, n_rows, bits, dev_i32(start), dev_i32(np.full(n_seq, length)), length, out,
+                          lse, None, 0)
+    values = O.packed_values(W.bf16_bits_to_f64(vb), bits)
+    want = np.stack([values[start + best[:, h], h] for h in range(hkv)], 1)
+    assert np.array_equal(f64_of(out)[:, 0], want)
+    score = ahead * 2.0 ** power
+    assert (np.abs(lse.cpu().numpy().astype(np.float64) - score) <= 2.0 ** -21 * abs(score)).all()
