@@ -439,9 +439,9 @@ ct_status ct_unpack_kv(const ct_layer_cfg* cfg, const void* cache, int32_t n_row
  * tokens among them (written before by ct_pack_kv); token t of them sees the first seq_len[b] - n_new + t + 1 rows:
  *   out[b,t,h,:] = sum_j softmax_j(q[b,t,h,:] . k_j,g * scale) v_j,g,  g = h / (n_q_heads / n_kv_heads).
  * bf16 operands (the cache's values are exact in bf16, a probability is a sum of two of them, off by up to 2^-16 of it),
- * fp32 scores / softmax / accumulation, which holds the largest values a cache has over 2^19 rows.  A token that sees no
- * row (an empty sequence, or n_new above its length) gets zeros and lse = -inf.  Rows outside a sequence do not reach its
- * results, whatever they hold, and neither do rows that a token does not see.
+ * fp32 scores (up to 2^28 in magnitude once scaled) / softmax / accumulation, which holds the largest values a cache has
+ * over 2^19 rows.  A token that sees no row (an empty sequence, or n_new above its length) gets zeros and lse = -inf.
+ * Rows outside a sequence do not reach its results, whatever they hold, and neither do rows that a token does not see.
  *   q, out     device bf16 [n_seq, n_new, n_q_heads, head_dim], 16-byte aligned; n_new in [1, 64]
  *   seq_start  device int32 [n_seq], any row of the cache
  *   seq_len    device int32 [n_seq], in [0, max_len]; larger ones are cut to max_len and to the end of the cache

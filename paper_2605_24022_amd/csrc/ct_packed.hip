@@ -2,7 +2,8 @@
 // their new positions (ct_unpack_kv; Eq. 8 in delta form, as for chunks cached in bf16).
 //
 // Bound: memory.  Both move every byte once: a token of 8 heads of 128 is 4096 bytes in bf16 (K and V) and 1088 in 4
-// bits, 2112 in 8.  32768 tokens to 4 bits and back: 59 us for 340 MB, 5.7 TB/s.
+// bits, 2112 in 8.  32768 tokens to 4 bits and back: 61 us for 340 MB, 5.6 TB/s.  Tokens that lie anywhere in the cache cost
+// more than their bytes: a row of one head is part of one line of K codes, two of V codes and two of scales in 4 bits.
 #include "ct_packed.h"
 #include "ct_rotate.h"
 
@@ -156,7 +157,8 @@ struct Packed8 {
 // A workgroup takes a tile of tokens (32, or 64 with heads of 64) and two heads.  K: a thread owns 8 rotation pairs of one
 // token, its sines and cosines serve both heads.  V: a thread takes 8 elements, threads along the tokens, the order of
 // the codes; both write whole lines.  One, two, four or eight heads per workgroup: 8192 tokens in 4 bits 9.5 / 8.0 / 8.2 /
-// 10.3 us (36 MB), 31901 in 8 bits 37 / 31.5 / 36 / 37 (169 MB, 5.4 TB/s; a large copy moves 5.1).
+// 10.3 us (36 MB), 31901 in 8 bits 37 / 31.5 / 36 / 37 when that was measured (now
+// 28.2 for 169 MB in turn over three inputs, 6.0 TB/s, 30.3 over four, 37.9 over six; a large copy moves 5.1).
 // The stores do not stay in the caches: 8.0 against 9.7 us, and 33.9 against 42.1 when that was measured; what follows in
 // a partial prefill takes about as much longer as the call gains (unpack, projection, scatter and attention of 15 % of
 // 31901 rows 1281 us with either, of 5 % 500 against 497; of 15 % of 8192 186.6 against 186.0).

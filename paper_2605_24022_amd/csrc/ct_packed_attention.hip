@@ -3,8 +3,9 @@
 //
 // Bound: the cache is read once and used for few queries, so memory decides as long as the conversion of the codes
 // keeps up: an element costs one conversion instruction per two, and V one v_perm per two besides.  64 sequences of
-// 4096 rows (32/8 heads of 128) 46 us in 4 bits, 6.2 TB/s; 2 of 131072 in 8 bits 85 us, 6.5 TB/s (a large copy moves
-// 5.1); short calls are a launch of 5 us, and a merge of 4 behind it where the key range is divided.
+// 4096 rows (32/8 heads of 128) 49 us in 4 bits, 5.8 TB/s; 2 of 131072 in 8 bits 85 us, 6.5 TB/s (a large copy moves
+// 5.1); short calls are a launch of 5 us, and a merge of 4 behind it where the key range is divided.  With more than 16
+// columns of queries the vector and matrix units decide: 16 sequences of 8192 rows with 64 columns 71 us in 4 bits.
 //
 // Formulation, as in the selected-row attention: S^T = K Q^T and O^T += V^T P^T on 16 x 16 x 32 matrix instructions,
 // the columns being the G query heads of a KV head times the new tokens.  The cache's layout hands a lane its
@@ -342,10 +343,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(NT 
       l_run[n] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       // bf16 operands: a probability is the sum of two, its rounding and the rounding of what that leaves, which is off by
       // up to 2^-16 of it; the sum above is unrounded.  (The first alone is off by up to 2^-8: outputs 0.0023 from the exact
-      // ones in relative 2-norm, where their own rounding makes 0.0017.  The second product costs 0 to 2 % where memory
-      // decides (64 uneven sequences up to 4099 rows 33.1 -> 33.4 us, 2 of 131072 in 8 bits 85.0 -> 85.2), 7 % of one
-      // sequence of 1024 rows with heads of 64 (5.35 -> 5.74) and up to 18 % where the vector and matrix units do: 16
-      // sequences of 8192 rows with 64 columns 58 -> 68, in 8 bits 75.5 -> 80.)
+      // ones in relative 2-norm, where their own rounding makes 0.0017.  The second product, 32/8 heads of 128: one token in
+      // 8 bits 0 to 1 %, in 4 bits 1 to 6 % (64 uneven sequences up to 4099 rows 32.9 -> 33.5 us, 64 of 4096 46.7 -> 49),
+      // one sequence of 1024 rows with heads of 64 5.35 -> 5.7, 64 columns over 16 sequences of 8192 rows 58 -> 71, in 8 bits
+      // 75.5 -> 81.  What the rounding leaves by a dot product of bf16 pairs instead of a shift and a difference: 2 % less of
+      // the slowest of these, as much of the others.)
       const u32x4 w = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
       pf[n] = __builtin_bit_cast(bf16x8, w);
       u32x4 rest;
@@ -535,20 +537,21 @@ __global__ __launch_bounds__(kMergeThreads) void packed_merge_kernel(PackedAttnA
     a.lse[row] = (top + __builtin_log2f(total)) * 0.69314718055994531f;
 }
 
-// Codes that are read once stream past the caches: 64 sequences of 4096 rows 50.8 -> 46.1 us in 4 bits (6.2 TB/s), of 2048
-// rows 48.4 -> 44.0 in 8, 2 of 131072 in 8 94.5 -> 85.4.  What several workgroups read suffers in 8 bits, not in 4: 16
-// sequences of 8192 rows with 64 columns in two workgroups 76.6 -> 92.1 (60.7 -> 59.1), 64 sequences that are the same
-// 32768 rows 304 -> 419 (215 -> 217).  So 8-bit codes stream where one workgroup holds all columns and the cache has
-// rows enough for no two sequences to share any.
+// Codes that are read once stream past the caches: 64 sequences of 4096 rows 52.4 -> 49.3 us in 4 bits (5.8 TB/s), of 2048
+// rows 48.3 -> 43.9 in 8, 2 of 131072 in 8 93.9 -> 84.9.  What several workgroups read suffers in 8 bits, not in 4: 16
+// sequences of 8192 rows with 64 columns in two workgroups 81 -> 93 (71 -> 71), 64 sequences that are the same 32768 rows
+// 308 -> 421 (243 -> 244).  So 8-bit codes stream where one workgroup holds all columns and the cache has rows enough for all
+// sequences at their longest, so that none need share any.  (Uneven sequences that lie one close behind the other in a
+// cache of no more rows than they have go through the caches too; where each lies is on the device.)
 bool stream_loads(int bits, int col_blocks, int64_t n_seq, int64_t max_len, int64_t n_rows) {
   return bits == 4 || (col_blocks == 1 && n_seq * max_len <= n_rows);
 }
 
 // Sequences to a round of by_length, or 0: taken as they come.  32/8 heads of 128, uneven lengths up to max_len, as they come
-// and by length: 64 sequences up to 4099 rows 35.5 -> 32.7 us in 4 bits (all of the mean length 31.5), 70.0 -> 61.9 in 8; 128
-// up to 4099 67.6 -> 63.8, 200 up to 3000 in 8 bits 146.0 -> 137.8.  A wave needs 0.6 us more for it, with more than 64
-// sequences 1.3, as much as is gained up to 2048 rows (64 sequences 18.9 and 18.8 us, 256 62.5 and 62.5; up to 1024 rows 128
-// sequences 21.3 and 22.4).
+// and by length: 64 sequences up to 4099 rows 38.2 -> 33.6 us in 4 bits (all of the mean length 33.3), 70.8 -> 62.2 in 8; 128
+// up to 4099 71.2 -> 66.4, 200 up to 3000 in 8 bits 146.8 -> 138.5.  A wave needs 0.6 us more for it, with more than 64
+// sequences 1.3, about as much as is gained up to 2048 rows (64 sequences 21.4 and 21.0 us, 256 66.4 and 64.8; up to 1024
+// rows 128 sequences 22.8 and 23.6).
 int round_of(int64_t workgroups, int64_t n_seq, int64_t max_len) {
   if (workgroups <= kNumCUs || n_seq > kOrdered || max_len <= 2048) return 0;
   return (int)std::max<int64_t>(kNumCUs * n_seq / workgroups, 1);
@@ -562,23 +565,25 @@ struct PackedPlan {
   size_t o_bytes, ws_bytes;
 };
 
-// How the key range is divided.  One wave takes about 0.5 us for a block of 32 rows (260 vector instructions at 4
-// cycles each; 0.36 with heads of 64) and the launch of the merge costs 3 us: sequences of up to 1024 rows stay
-// whole (one token, 32/8 heads of 128, 1, 4 and 16 sequences of 1024 rows: 7.7, 8.3 and 8.5 us whole, 8.1, 8.7 and
-// 10.5 in parts; 8/2 heads of 64 5.7 and 7.7; one of 2048 rows 12.6 and 8.5, 8.5 and 7.6).
+// How the key range is divided.  A wave alone takes about 0.64 us for a block of 32 rows (219 instructions with 4 bits, 211
+// with 8, and the latency of its loads; 0.46 with heads of 64) and the merge's launch 4 us: sequences of up to 1024 rows stay
+// whole (one token, 32/8 heads of 128, 1, 4 and 16 sequences of 1024 rows: 7.5, 8.2 and 8.5 us whole, 7.4, 8.4 and 10.3
+// in parts; 8/2 heads of 64 5.6, 6.0 and 6.6, and 6.7 to 7.4, 7.1 to 7.5 and 7.7; of 2048 rows 12.6, 12.9 and 13.4, and 8.0, 8.5
+// and 12.9; 9.2, 9.6 and 10.2, and 7.1, 7.4 and 7.8).  The lines cross between 1024 rows (one sequence of heads of 128), 1300
+// to 1500 (heads of 64) and 1800 (16 sequences of heads of 128): up to there calls pay up to 1.8 us more than whole.
 // Longer ones are divided until a workgroup stands on each compute unit, into parts of at least 128 rows; where
 // parts would be longer than 4096 rows, until two do, because sequences of uneven length leave units idle for as long
-// as a part takes.  256 / 512 workgroups, 32/8 heads of 128, 4 bits, one token: one sequence of 8192 rows 10.4 / 10.5 us,
-// of 32768 13.0 / 14.6, of 65536 18.1 / 19.8; four of 8192 12.8 / 13.5, of 32768 28.3 / 29.0, two of 131072 in 8 bits
-// 83.6 / 85.3; but eight of 4096 to 16384 rows with four tokens 29.7 / 26.9.  Never a few more than fit, and two or three to
+// as a part takes.  256 / 512 workgroups, 32/8 heads of 128, 4 bits, one token: one sequence of 8192 rows 10.0 / 10.1 us,
+// of 32768 12.9 / 14.6, of 65536 18.0 / 19.7; four of 8192 12.6 / 13.4, of 32768 28.7 / 28.7, two of 131072 in 8 bits
+// 83.4 / 84.7; but eight of 4096 to 16384 rows with four tokens 29.0 / 26.8.  Never a few more than fit, and two or three to
 // a unit where fewer would leave places empty (as many parts as reach 256 or 512 workgroups / this rule: 5 sequences of
-// 65536 rows 71.8 / 57.7 us, 9 of up to 4099 14.1 / 12.4, 12 16.8 / 13.8, in 8 bits 25.9 / 20.9, 24 of up to 8192 36.3 / 31.5;
-// the worst, 13 of up to 16384, 32.5 / 35.5).  Three fit a unit, and are slower where two fill it (64 sequences of 4096 rows
-// 46 us with 512 workgroups, 52 with 768).
+// 65536 rows 76 / 61 us, 9 of up to 4099 15.3 / 13.1, 12 18.5 / 14.4, in 8 bits 26.2 / 21.2, 24 of up to 8192 37.9 / 33.1;
+// the worst, 13 of up to 16384, 33.5 / 36.9).  Three to a unit are slower where two fill it (32 sequences of 8192 rows 51 us
+// with 512 workgroups, 52.3 with 768), and more are not planned for, though a unit holds four with heads of 64.
 // More whole sequences than units are not divided in two: taken by length they share the units well, and no merge is needed
-// (uneven lengths, divided / whole: 36 sequences up to 4099 rows 29.9 / 25.2 us, 56 38.3 / 30.0, 60 up to 16384 134 / 111, in 8
-// bits 252 / 219), except long ones that leave more than half of the units with one workgroup alone (33 of 16384 rows 80.4
-// / 84.1, in 8 bits 162 / 163 and 153 / 179 where all are as long; 48 99.2 / 96.9 and 192 / 190).
+// (uneven lengths, divided / whole: 36 sequences up to 4099 rows 31.3 / 25.8 us, 48 up to 16384 102.8 / 97.6, in 8 bits 192 /
+// 190), except long ones that leave more than half of the units with one workgroup alone (33 up to 16384 rows 91.6 / 94.7,
+// in 8 bits 162 / 163 and 219 / 265 where all are as long).
 PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, int64_t max_len) {
   PackedPlan p;
   const int64_t n_cols = n_new * (cfg->n_q_heads / cfg->n_kv_heads);
@@ -587,7 +592,7 @@ PackedPlan plan_packed(const ct_layer_cfg* cfg, int64_t n_seq, int64_t n_new, in
   const int64_t blocks = (max_len + kPackRows - 1) / kPackRows + 1;   // a sequence may start inside a block
   const int64_t groups = n_seq * cfg->n_kv_heads * p.col_blocks;
   int64_t parts[4], used[4];      // where k workgroups stand on a unit: parts of a sequence, sixteenths of the places that are taken
-  const int fit = p.col_tiles == 1 ? 3 : 2;      // what a unit holds with heads of 128 (4 and 3 with heads of 64)
+  const int fit = p.col_tiles == 1 ? 3 : 2;      // what a unit holds with heads of 128
   for (int k = 1; k <= fit; ++k) {
     parts[k] = std::max<int64_t>(k * kNumCUs / groups, 1);
     used[k] = std::min<int64_t>(16 * groups * parts[k] / (k * kNumCUs), 16);

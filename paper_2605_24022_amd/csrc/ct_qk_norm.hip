@@ -3,7 +3,8 @@
 //
 //   y = x / sqrt(mean(x^2) + eps) * w over the D elements of a head, then RoPE at the token's position; v is copied.
 // fp32 from the bf16 input to the one rounding of the result.  Bound: memory, each element read and written once: 4915
-// rows of 32 + 8 + 8 heads of 128, 121 MB, 22.2 us (5.5 TB/s; a large copy reaches 5.1); 7 rows 4.6 us, the launch.
+// rows of 32 + 8 + 8 heads of 128, 121 MB, 22.4 us (5.4 TB/s; a large copy reaches 5.1) in turn over six inputs, 19.0 over
+// four or fewer; 7 rows 4.5 to 5.2 us, the launch.
 #include <math.h>
 
 #include "ct_internal.h"
